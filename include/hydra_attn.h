@@ -493,12 +493,100 @@ int32_t hydra_gate_apply_bwd(const void* dy, const void* out, const void* gate, 
                              void* d_gate, void* cuda_stream);
 
 /*
+ * Rotary positions with several axes (time, height, width of a video's patches; row and column of an image's). The paper
+ * trains on text with one position per token (hydra_mla_rope); this is the same rotation for tokens that have up to
+ * HYDRA_MAX_AXES positions. hydra_rope_t says which columns of a head are rotary and which axis a rotary pair follows:
+ *   the columns [offset, offset + dim) are rotated in pairs (2i, 2i+1); the first axis_pairs[0] pairs follow axis 0, the next
+ *   axis_pairs[1] axis 1, and so on (together dim / 2 pairs; an axis may have none); pair i turns by the angle
+ *   positions[axis(i), t] * theta^(-2i / dim), i counted over all axes, so that a token whose positions are all equal is
+ *   rotated as by hydra_mla_rope, bit for bit.
+ *   x device bf16, y device bf16: the row of head a of token t begins at element t * stride + a * head_dim (x_stride, y_stride
+ *   >= n_heads * head_dim: x may be a slice of a fused projection's output); positions device int32 [n_axes, n_tokens].
+ *   inverse != 0 rotates by the opposite angles: the gradient of the step. y == x (with equal strides) rotates in place;
+ *   otherwise the two must not overlap, and the other columns are copied.
+ * One launch on cuda_stream, bound by HBM: every byte moves once (in place: the rotary ones). fp32 arithmetic, angles in double precision,
+ * one rounding per element.
+ * Requirements: head_dim <= 1024, offset, dim <= 256 and the strides multiples of 8 elements, n_heads <= 65536, x and y 16-byte
+ * aligned (else HYDRA_ERR_UNSUPPORTED for the multiples and limits, HYDRA_ERR_INVALID_ARG for pointers); theta > 1.
+ */
+#define HYDRA_MAX_AXES 4
+typedef struct hydra_rope_t {
+    float theta;
+    int32_t offset, dim;
+    int32_t n_axes;                       /* 1 .. HYDRA_MAX_AXES                                        */
+    int32_t axis_pairs[HYDRA_MAX_AXES];   /* rotary pairs of every axis; entries from n_axes on ignored */
+} hydra_rope_t;
+int32_t hydra_rope_axes(const void* x, int64_t x_stride, const int32_t* positions, int64_t n_tokens, int32_t n_heads,
+                        int32_t head_dim, const hydra_rope_t* rope, int32_t inverse, void* y, int64_t y_stride,
+                        void* cuda_stream);
+
+/*
+ * Generating with the trained model: a paged key / value cache, the step that appends to it, and the attention of one new
+ * token per sequence over it (the paper trains only; its model is evaluated with these). The cache is the caller's memory:
+ *   k, v        device bf16 [n_pages, n_kv_heads, page_size, d_qk] and [n_pages, n_kv_heads, page_size, d_v]: a page holds
+ *               page_size consecutive tokens of one sequence, head by head. 16-byte aligned.
+ *   page_table  device int32 [n_seqs, max_pages]: entry j of row b is the page of tokens [j * page_size, (j + 1) * page_size)
+ *               of sequence b. An entry outside [0, n_pages) is a page that is not there (never given out, or taken back):
+ *               nothing is written to it and no key of it is seen. A page may be shared by sequences that read it; new tokens
+ *               of two sequences must not go to one place.
+ *   seq_lens    device int32 [n_seqs]: tokens of each sequence INCLUDING those that are being appended. 0 is an empty row (a
+ *               padded batch). Lengths beyond max_pages * page_size: the tokens behind that have no place; negative counts as 0.
+ * The struct is host memory, read during the call. Lengths, table and cache contents are read on the device when the kernels
+ * run: a captured call follows them, and neither call waits for the device or copies to the host.
+ *
+ * hydra_kv_append: token t of the n_tokens rows of k, v is one of the new tokens of a sequence: of sequence b for cu_new[b] <=
+ * t < cu_new[b + 1], and with n = cu_new[b + 1] - cu_new[b] new tokens it is token seq_lens[b] - n + (t - cu_new[b]) of that
+ * sequence. Its key row of every head is rotated as by hydra_rope_axes and stored, its value row stored; all other rows of the cache
+ * stay as they are.
+ *   k, v        device bf16: head a of token t at element t * k_stride + a * d_qk and t * v_stride + a * d_v.
+ *   positions   device int32 [rope->n_axes, n_tokens]; NULL with one axis: the token's index in its sequence.
+ *   cu_new      device int32 [n_seqs + 1], non-decreasing from 0; NULL: row b is the one new token of sequence b. Rows behind
+ *               the last sequence, and tokens without a place (an index below 0, behind the table's end, on a page that is not
+ *               there), are skipped.
+ *   rope        host; NULL stores the keys as they are.
+ * hydra_mla_kv_append: the same from the KV up-projection of an MLA block, without k and v in between: kv_up has, per token
+ * and head, [d_qk - rope->dim key columns | d_v value columns] (heads contiguous, tokens kv_up_stride elements apart), k_pe
+ * one rotary key of rope->dim columns per token for all heads (tokens k_pe_stride elements apart); rope->offset must be d_qk -
+ * rope->dim. The stored rows are those of hydra_mla_kv_assemble.
+ * One launch each, bound by HBM: every byte moves once. Requirements: as for hydra_rope_axes, with d_qk and d_v <= 1024
+ * multiples of 8 and a k_pe stride that is even (k_pe 4-byte aligned).
+ *
+ * hydra_attn_decode: for every sequence b and query head a,
+ *   s_j = softmax_scale * <q[b, a], k_j> over the positions j < seq_lens[b] whose page is there, of KV head a / (n_heads /
+ *   n_kv_heads);  lse[a, b] = ln sum_j exp(s_j),  out[b, a] = sum_j exp(s_j - lse) v_j   (no position: out = 0, lse = -inf).
+ *   q           device bf16: head a of sequence b at element b * q_stride + a * d_qk (q_stride a multiple of 8).
+ *   out, lse    device bf16 [n_seqs, n_heads, d_v], fp32 [n_heads, n_seqs]: an (out, lse) as of hydra_attn_fwd, with n_seqs
+ *               tokens; hydra_lse_merge_accumulate merges it with others.
+ *   workspace   device, >= hydra_workspace_bytes_decode(n_heads, n_kv_heads) bytes, 16-byte aligned; whatever it held before.
+ * Cached rows that do not count (behind a sequence's end, on pages of others) may hold anything, infinities and NaN too; q and
+ * the rows that count must be finite. Scores, softmax and sums in fp32, probabilities enter the product with v in 16 bits of precision, one
+ * rounding of out; the result does not depend on timing, and the sequences' lengths decide how the work is split.
+ * Two launches. (d_qk, d_v) = (192, 128) or (128, 128), page_size a multiple of 8, n_pages * n_kv_heads * page_size < 2^31
+ * (else HYDRA_ERR_UNSUPPORTED). A wait in the kernel that runs out leaves HYDRA_ERR_DEVICE_TIMEOUT in the workspace's status.
+ */
+typedef struct hydra_paged_cache_t {
+    void *k, *v;
+    const int32_t *page_table, *seq_lens;
+    int32_t n_pages, page_size, n_kv_heads, d_qk, d_v;
+    int32_t n_seqs, max_pages;
+} hydra_paged_cache_t;
+int32_t hydra_kv_append(const void* k, int64_t k_stride, const void* v, int64_t v_stride, const int32_t* positions,
+                        const int32_t* cu_new, int64_t n_tokens, const hydra_rope_t* rope, const hydra_paged_cache_t* cache,
+                        void* cuda_stream);
+int32_t hydra_mla_kv_append(const void* kv_up, int64_t kv_up_stride, const void* k_pe, int64_t k_pe_stride,
+                            const int32_t* positions, const int32_t* cu_new, int64_t n_tokens, const hydra_rope_t* rope,
+                            const hydra_paged_cache_t* cache, void* cuda_stream);
+size_t hydra_workspace_bytes_decode(int32_t n_heads, int32_t n_kv_heads);
+int32_t hydra_attn_decode(const void* q, int64_t q_stride, const hydra_paged_cache_t* cache, int32_t n_heads,
+                          float softmax_scale, void* out, float* lse, void* workspace, size_t workspace_bytes,
+                          void* cuda_stream);
+
+/*
  * Per-kernel timing (measurement aid, not part of the method). While enabled, every kernel launch
  * is bracketed by CUDA events on its stream. hydra_profile_collect waits for the recorded events,
  * adds their durations into ms_out[8] and their counts into launches_out[8] (index: 0 forward, both of its
- * kernels when a call uses both,
- * 1 merge, 2 backward prep, 3 backward dK/dV, 4 backward dQ, 5 gradient cast, 6 Ulysses pack / unpack,
- * 7 the elementwise steps of the gated MLA block)
+ * kernels when a call uses both, and hydra_attn_decode, 1 merge, and the join of hydra_attn_decode, 2 backward prep, 3 backward dK/dV, 4 backward dQ, 5 gradient cast, 6 Ulysses pack / unpack,
+ * 7 the elementwise steps of the gated MLA block, hydra_rope_axes and the appends to a paged cache)
  * and forgets them.
  */
 void hydra_profile_enable(int32_t on);
@@ -551,6 +639,7 @@ void hydra_set_wait_limit_ns(uint64_t ns);
 #define HYDRA_STALL_FWD 0       /* either forward kernel */
 #define HYDRA_STALL_BWD_DKV 1
 #define HYDRA_STALL_BWD_DQ 2    /* either form of the query-side kernel */
+#define HYDRA_STALL_DECODE 3
 void hydra_debug_stall(int32_t kernel, uint64_t ns);
 
 int32_t hydra_version(void);

@@ -40,6 +40,44 @@ PAIR_DTYPE = np.dtype([("seq", "<i4"), ("q_start", "<i4"), ("q_len", "<i4"), ("k
 CHUNK_DTYPE = np.dtype([("seq", "<i4"), ("start", "<i4"), ("len", "<i4"), ("row", "<i4")])
 
 
+HYDRA_MAX_AXES = 4
+
+
+class hydra_rope_t(ctypes.Structure):
+    _fields_ = [("theta", ctypes.c_float), ("offset", ctypes.c_int32), ("dim", ctypes.c_int32), ("n_axes", ctypes.c_int32),
+                ("axis_pairs", ctypes.c_int32 * HYDRA_MAX_AXES)]
+
+
+class hydra_paged_cache_t(ctypes.Structure):
+    _fields_ = [("k", ctypes.c_void_p), ("v", ctypes.c_void_p), ("page_table", ctypes.c_void_p), ("seq_lens", ctypes.c_void_p),
+                ("n_pages", ctypes.c_int32), ("page_size", ctypes.c_int32), ("n_kv_heads", ctypes.c_int32),
+                ("d_qk", ctypes.c_int32), ("d_v", ctypes.c_int32), ("n_seqs", ctypes.c_int32), ("max_pages", ctypes.c_int32)]
+
+
+def rope_spec(theta: float, dim: int, offset: int = 0, axis_pairs: Optional[Sequence[int]] = None) -> hydra_rope_t:
+    """Which columns of a head are rotary, and the rotary pairs of every axis (None: one axis has them all)."""
+    pairs = [dim // 2] if axis_pairs is None else [int(n) for n in axis_pairs]
+    if len(pairs) > HYDRA_MAX_AXES:
+        raise ValueError(f"at most {HYDRA_MAX_AXES} axes")
+    return hydra_rope_t(float(theta), int(offset), int(dim), len(pairs), (ctypes.c_int32 * HYDRA_MAX_AXES)(*pairs))
+
+
+def paged_cache(k, v, page_table, seq_lens) -> hydra_paged_cache_t:
+    """The description of a paged cache of CUDA tensors: k [n_pages, n_kv_heads, page_size, d_qk] and v [.., d_v] bf16,
+    page_table [n_seqs, max_pages] and seq_lens [n_seqs] int32. It keeps the tensors alive and may be used for many calls; the
+    tensors' contents are read when a call's kernels run."""
+    if k.dim() != 4 or v.dim() != 4 or k.shape[:3] != v.shape[:3]:
+        raise ValueError("k and v are [n_pages, n_kv_heads, page_size, d], alike but for d")
+    if page_table.dim() != 2 or tuple(seq_lens.shape) != (page_table.shape[0],):
+        raise ValueError("page_table is [n_seqs, max_pages], seq_lens [n_seqs]")
+    if any(str(t.dtype) != "torch.bfloat16" for t in (k, v)) or any(str(t.dtype) != "torch.int32" for t in (page_table, seq_lens)):
+        raise ValueError("k and v are bf16, page_table and seq_lens int32")
+    c = hydra_paged_cache_t(_ptr(k), _ptr(v), _ptr(page_table), _ptr(seq_lens), k.shape[0], k.shape[2], k.shape[1], k.shape[3],
+                            v.shape[3], page_table.shape[0], page_table.shape[1])
+    c.tensors = (k, v, page_table, seq_lens)
+    return c
+
+
 def as_chunks(chunks) -> np.ndarray:
     """A chunk table (include/hydra_attn.h, hydra_chunk_t): structured array, or an iterable of (seq, start, len, row)."""
     if isinstance(chunks, np.ndarray) and chunks.dtype == CHUNK_DTYPE:
@@ -158,6 +196,16 @@ def _load() -> ctypes.CDLL:
     lib.hydra_gate_apply.argtypes = [vp, vp, i64, vp, vp]
     lib.hydra_gate_apply_bwd.restype = i32
     lib.hydra_gate_apply_bwd.argtypes = [vp, vp, vp, i64, vp, vp, vp]
+    lib.hydra_rope_axes.restype = i32
+    lib.hydra_rope_axes.argtypes = [vp, i64, vp, i64, i32, i32, vp, i32, vp, i64, vp]
+    lib.hydra_kv_append.restype = i32
+    lib.hydra_kv_append.argtypes = [vp, i64, vp, i64, vp, vp, i64, vp, vp, vp]
+    lib.hydra_mla_kv_append.restype = i32
+    lib.hydra_mla_kv_append.argtypes = [vp, i64, vp, i64, vp, vp, i64, vp, vp, vp]
+    lib.hydra_workspace_bytes_decode.restype = sz
+    lib.hydra_workspace_bytes_decode.argtypes = [i32, i32]
+    lib.hydra_attn_decode.restype = i32
+    lib.hydra_attn_decode.argtypes = [vp, i64, vp, i32, f32, vp, vp, vp, sz, vp]
     lib.hydra_poll_status.restype = i32
     lib.hydra_poll_status.argtypes = [vp, vp, vp, vp]
     lib.hydra_poll_clocks.restype = i32
@@ -189,7 +237,8 @@ EXPORTS = ("hydra_version", "hydra_status_string", "hydra_launch_count", "hydra_
            "hydra_mla_rope", "hydra_mla_kv_assemble", "hydra_mla_kv_assemble_bwd", "hydra_gate_apply", "hydra_gate_apply_bwd",
            "hydra_attn_fwd_local", "hydra_lse_merge_local", "hydra_attn_bwd_accumulate_local", "hydra_workspace_bytes_local",
            "hydra_attn_fwd_dims", "hydra_attn_bwd_dims", "hydra_attn_bwd_accumulate_dims", "hydra_workspace_bytes_dims",
-           "hydra_poll_clocks")
+           "hydra_poll_clocks",
+           "hydra_rope_axes", "hydra_kv_append", "hydra_mla_kv_append", "hydra_attn_decode", "hydra_workspace_bytes_decode")
 KERNEL_KINDS = ("fwd", "merge", "bwd_prep", "bwd_dkv", "bwd_dq", "grad_cast", "ulysses", "mla_ops")
 
 
@@ -290,7 +339,7 @@ def hydra_set_wait_limit_ns(ns: int) -> None:
     _lib.hydra_set_wait_limit_ns(int(ns))
 
 
-HYDRA_STALL_FWD, HYDRA_STALL_BWD_DKV, HYDRA_STALL_BWD_DQ = 0, 1, 2
+HYDRA_STALL_FWD, HYDRA_STALL_BWD_DKV, HYDRA_STALL_BWD_DQ, HYDRA_STALL_DECODE = 0, 1, 2, 3
 
 
 def hydra_debug_stall(kernel: int, ns: int) -> None:
@@ -641,6 +690,77 @@ def hydra_gate_apply_bwd(dy, out, gate, n_elements: int, d_out, d_gate, stream=N
                                   _stream(stream))
     if check:
         _check(s, "hydra_gate_apply_bwd")
+    return s
+
+
+def _rows(x, stride: Optional[int]) -> Tuple[Optional[int], int]:
+    """(device pointer, elements between tokens) of rows that are contiguous but for the distance between tokens: a tensor
+    [tokens, ...], possibly a slice of a wider one, or a raw pointer with its stride."""
+    if x is None or isinstance(x, int):
+        return x, 0 if stride is None else int(stride)
+    want = 1
+    for size, step in zip(reversed(x.shape[1:]), reversed(x.stride()[1:])):
+        if size != 1 and step != want:
+            raise ValueError("a token's rows must be contiguous")
+        want *= size
+    if not x.is_cuda:
+        raise ValueError("tensors must be CUDA tensors")
+    return x.data_ptr(), int(stride) if stride is not None else x.stride(0) if x.shape[0] > 1 else max(want, x.stride(0))
+
+
+def _spec(x) -> Optional[int]:
+    return None if x is None else ctypes.addressof(x)
+
+
+def hydra_rope_axes(x, positions, n_tokens: int, n_heads: int, head_dim: int, rope: hydra_rope_t, inverse: bool, y,
+                    x_stride: Optional[int] = None, y_stride: Optional[int] = None, stream=None, check: bool = True) -> int:
+    """Rotary embedding with a position per axis (positions [n_axes, n_tokens] int32); the tokens of x and y may be apart."""
+    (xp, xs), (yp, ys) = _rows(x, x_stride), _rows(y, y_stride)
+    s = _lib.hydra_rope_axes(xp, xs, _ptr(positions), int(n_tokens), n_heads, head_dim, _spec(rope), int(bool(inverse)), yp, ys,
+                             _stream(stream))
+    if check:
+        _check(s, "hydra_rope_axes")
+    return s
+
+
+def hydra_kv_append(k, v, positions, cu_new, n_tokens: int, rope: Optional[hydra_rope_t], cache: hydra_paged_cache_t,
+                    k_stride: Optional[int] = None, v_stride: Optional[int] = None, stream=None, check: bool = True) -> int:
+    """New tokens' keys, rotated, and values into the paged cache. cu_new None: one new token of every sequence."""
+    (kp, ks), (vp, vs) = _rows(k, k_stride), _rows(v, v_stride)
+    s = _lib.hydra_kv_append(kp, ks, vp, vs, _ptr(positions), _ptr(cu_new), int(n_tokens), _spec(rope), _spec(cache),
+                             _stream(stream))
+    if check:
+        _check(s, "hydra_kv_append")
+    return s
+
+
+def hydra_mla_kv_append(kv_up, k_pe, positions, cu_new, n_tokens: int, rope: hydra_rope_t, cache: hydra_paged_cache_t,
+                        kv_up_stride: Optional[int] = None, k_pe_stride: Optional[int] = None, stream=None,
+                        check: bool = True) -> int:
+    """The same from the KV up-projection and the rotary key that all heads share (as in hydra_mla_kv_assemble)."""
+    (up, us), (pe, ps) = _rows(kv_up, kv_up_stride), _rows(k_pe, k_pe_stride)
+    s = _lib.hydra_mla_kv_append(up, us, pe, ps, _ptr(positions), _ptr(cu_new), int(n_tokens), _spec(rope), _spec(cache),
+                                 _stream(stream))
+    if check:
+        _check(s, "hydra_mla_kv_append")
+    return s
+
+
+def hydra_workspace_bytes_decode(n_heads: int, n_kv_heads: int) -> int:
+    return int(_lib.hydra_workspace_bytes_decode(int(n_heads), int(n_kv_heads)))
+
+
+def hydra_attn_decode(q, cache: hydra_paged_cache_t, n_heads: int, softmax_scale: float, out, lse, workspace,
+                      workspace_bytes: Optional[int] = None, q_stride: Optional[int] = None, stream=None,
+                      check: bool = True) -> int:
+    """Attention of one new token per sequence (q [n_seqs, n_heads, d_qk]) over the paged cache, split over its length."""
+    if workspace_bytes is None:
+        workspace_bytes = workspace.nbytes
+    qp, qs = _rows(q, q_stride)
+    s = _lib.hydra_attn_decode(qp, qs, _spec(cache), int(n_heads), float(softmax_scale), _ptr(out), _ptr(lse), _ptr(workspace),
+                               int(workspace_bytes), _stream(stream))
+    if check:
+        _check(s, "hydra_attn_decode")
     return s
 
 

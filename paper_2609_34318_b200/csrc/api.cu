@@ -21,7 +21,7 @@ namespace {
 
 std::atomic<int64_t> g_launches{0};
 std::atomic<uint64_t> g_wait_limit_ns{2000000000ull};
-std::atomic<uint64_t> g_debug_stall_ns[3];           // test hook, see hydra_debug_stall
+std::atomic<uint64_t> g_debug_stall_ns[4];           // test hook, see hydra_debug_stall
 
 constexpr size_t kStatusBytes = 256;
 
@@ -1582,7 +1582,7 @@ void hydra_set_wait_limit_ns(uint64_t ns) { g_wait_limit_ns.store(ns ? ns : 1); 
 
 void hydra_debug_stall(int32_t kernel, uint64_t ns)
 {
-    if (kernel >= 0 && kernel < 3) g_debug_stall_ns[kernel].store(ns);
+    if (kernel >= 0 && kernel < 4) g_debug_stall_ns[kernel].store(ns);
 }
 
 void hydra_shutdown(void)
@@ -2859,6 +2859,204 @@ int32_t hydra_gate_apply_bwd(const void* dy, const void* out, const void* gate, 
     cudaStream_t stream = static_cast<cudaStream_t>(cuda_stream);
     ScopedKernelTimer timer(K_MLA, stream);
     if (launch_gate_bwd(dy, out, gate, d_out, d_gate, n_elements / 8, stream) != cudaSuccess) return HYDRA_ERR_CUDA;
+    g_launches += 1;
+    return HYDRA_OK;
+}
+
+// ---------------------------------------------------------------------------------------------
+// rotary positions with several axes, the paged cache
+// ---------------------------------------------------------------------------------------------
+namespace {
+constexpr int32_t kMaxPlacedDim = 1024, kMaxPlacedHeads = 65536;
+
+// of the rotary columns of rows of head_dim elements
+int32_t check_rope(const hydra_rope_t* r, int32_t head_dim)
+{
+    if (!r || r->n_axes < 1 || r->n_axes > HYDRA_MAX_AXES || r->offset < 0 || r->dim < 2 || r->dim % 2 ||
+        int64_t{r->offset} + r->dim > head_dim || !(r->theta > 1.f) || !std::isfinite(r->theta))
+        return HYDRA_ERR_INVALID_ARG;
+    int64_t pairs = 0;
+    for (int a = 0; a < r->n_axes; ++a) {
+        if (r->axis_pairs[a] < 0) return HYDRA_ERR_INVALID_ARG;
+        pairs += r->axis_pairs[a];
+    }
+    if (pairs != r->dim / 2) return HYDRA_ERR_INVALID_ARG;
+    return r->offset % 8 || r->dim % 8 || r->dim > 256 ? HYDRA_ERR_UNSUPPORTED : HYDRA_OK;
+}
+
+int32_t check_cache(const hydra_paged_cache_t* c)
+{
+    if (!c || c->n_pages < 1 || c->page_size < 1 || c->n_kv_heads < 1 || c->d_qk < 1 || c->d_v < 1 || c->n_seqs < 0 || c->max_pages < 1)
+        return HYDRA_ERR_INVALID_ARG;
+    return HYDRA_OK;
+}
+int32_t check_cache_pointers(const hydra_paged_cache_t* c)
+{
+    if (!c->k || !c->v || !c->page_table || !c->seq_lens || !aligned16(c->k) || !aligned16(c->v) || !aligned4(c->page_table) ||
+        !aligned4(c->seq_lens))
+        return HYDRA_ERR_INVALID_ARG;
+    return HYDRA_OK;
+}
+
+// The checks that both forms of the append share. row_elems: elements of a token in k (kv_up).
+int32_t append_impl(const void* k, int64_t k_stride, int64_t row_elems, const void* v, int64_t v_stride, const void* pe, int64_t pe_stride,
+                    const int32_t* positions, const int32_t* cu_new, int64_t n_tokens, const hydra_rope_t* rope,
+                    const hydra_paged_cache_t* c, bool mla, void* cuda_stream)
+{
+    if (n_tokens < 0 || k_stride < row_elems) return HYDRA_ERR_INVALID_ARG;
+    if (c->d_qk > kMaxPlacedDim || c->d_v > kMaxPlacedDim || c->d_qk % 8 || c->d_v % 8 || c->n_kv_heads > kMaxPlacedHeads ||
+        k_stride % 8 || (!mla && v_stride % 8) || (mla && pe_stride % 2))
+        return HYDRA_ERR_UNSUPPORTED;
+    if (n_tokens == 0 || c->n_seqs == 0) return HYDRA_OK;
+    if (int32_t s = check_cache_pointers(c)) return s;
+    if (!k || !aligned16(k) || (mla ? !pe || !aligned4(pe) : !v || !aligned16(v))) return HYDRA_ERR_INVALID_ARG;
+    if (rope && (positions ? !aligned4(positions) : rope->n_axes != 1)) return HYDRA_ERR_INVALID_ARG;
+    if (!aligned4(cu_new)) return HYDRA_ERR_INVALID_ARG;
+    if (int32_t s = device_info(nullptr)) return s;
+    cudaStream_t stream = static_cast<cudaStream_t>(cuda_stream);
+    ScopedKernelTimer timer(K_MLA, stream);
+    if (launch_kv_append(k, k_stride, v, v_stride, pe, pe_stride, positions, cu_new, n_tokens, rope, *c, stream) != cudaSuccess)
+        return HYDRA_ERR_CUDA;
+    g_launches += 1;
+    return HYDRA_OK;
+}
+
+// rows of d bf16 as a 2-D map; a box is 64 columns of `rows` rows, written as 128-byte rows with the 128-byte swizzle
+int32_t make_rows_map(CUtensorMap* map, const void* base, int64_t n_rows, int32_t d, int32_t rows)
+{
+    EncodeFn enc = encode_fn();
+    if (!enc) return HYDRA_ERR_CUDA;
+    const cuuint64_t dims[2] = {static_cast<cuuint64_t>(d), static_cast<cuuint64_t>(n_rows)};
+    const cuuint64_t strides[1] = {static_cast<cuuint64_t>(d) * 2};
+    const cuuint32_t box[2] = {64, static_cast<cuuint32_t>(rows)};
+    const cuuint32_t es[2] = {1, 1};
+    const CUresult r = enc(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, const_cast<void*>(base), dims, strides, box, es,
+                           CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+                           CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+    return r == CUDA_SUCCESS ? HYDRA_OK : HYDRA_ERR_CUDA;
+}
+
+size_t decode_part_o_bytes(int32_t group)
+{
+    return size_t{2} * DECODE_MAX_BLOCKS * decode_rows_per_chunk(group) * D_V * sizeof(float);
+}
+}  // namespace
+
+int32_t hydra_rope_axes(const void* x, int64_t x_stride, const int32_t* positions, int64_t n_tokens, int32_t n_heads,
+                        int32_t head_dim, const hydra_rope_t* rope, int32_t inverse, void* y, int64_t y_stride, void* cuda_stream)
+{
+    if (n_tokens < 0 || n_heads < 1 || head_dim < 1) return HYDRA_ERR_INVALID_ARG;
+    const int32_t bad = check_rope(rope, head_dim);
+    if (bad == HYDRA_ERR_INVALID_ARG) return bad;
+    const int64_t row = int64_t{n_heads} * head_dim;
+    if (x_stride < row || y_stride < row || (x == y && x_stride != y_stride)) return HYDRA_ERR_INVALID_ARG;
+    if (bad || head_dim % 8 || head_dim > kMaxPlacedDim || n_heads > kMaxPlacedHeads || x_stride % 8 || y_stride % 8)
+        return HYDRA_ERR_UNSUPPORTED;
+    if (n_tokens == 0) return HYDRA_OK;
+    if (!x || !y || !positions || !aligned16(x) || !aligned16(y) || !aligned4(positions)) return HYDRA_ERR_INVALID_ARG;
+    if (int32_t s = device_info(nullptr)) return s;
+    cudaStream_t stream = static_cast<cudaStream_t>(cuda_stream);
+    ScopedKernelTimer timer(K_MLA, stream);
+    if (launch_rope_axes(x, x_stride, positions, n_tokens, n_heads, head_dim, *rope, inverse != 0, y, y_stride, stream) != cudaSuccess)
+        return HYDRA_ERR_CUDA;
+    g_launches += 1;
+    return HYDRA_OK;
+}
+
+int32_t hydra_kv_append(const void* k, int64_t k_stride, const void* v, int64_t v_stride, const int32_t* positions,
+                        const int32_t* cu_new, int64_t n_tokens, const hydra_rope_t* rope, const hydra_paged_cache_t* cache,
+                        void* cuda_stream)
+{
+    if (int32_t s = check_cache(cache)) return s;
+    const int32_t bad = rope ? check_rope(rope, cache->d_qk) : HYDRA_OK;
+    if (bad) return bad;
+    if (v_stride < int64_t{cache->n_kv_heads} * cache->d_v) return HYDRA_ERR_INVALID_ARG;
+    return append_impl(k, k_stride, int64_t{cache->n_kv_heads} * cache->d_qk, v, v_stride, nullptr, 0, positions, cu_new, n_tokens, rope,
+                       cache, false, cuda_stream);
+}
+
+int32_t hydra_mla_kv_append(const void* kv_up, int64_t kv_up_stride, const void* k_pe, int64_t k_pe_stride,
+                            const int32_t* positions, const int32_t* cu_new, int64_t n_tokens, const hydra_rope_t* rope,
+                            const hydra_paged_cache_t* cache, void* cuda_stream)
+{
+    if (int32_t s = check_cache(cache)) return s;
+    if (int32_t s = check_rope(rope, cache->d_qk)) return s;
+    if (rope->offset != cache->d_qk - rope->dim || k_pe_stride < rope->dim) return HYDRA_ERR_INVALID_ARG;
+    return append_impl(kv_up, kv_up_stride, int64_t{cache->n_kv_heads} * (rope->offset + cache->d_v), nullptr, 0, k_pe, k_pe_stride,
+                       positions, cu_new, n_tokens, rope, cache, true, cuda_stream);
+}
+
+size_t hydra_workspace_bytes_decode(int32_t n_heads, int32_t n_kv_heads)
+{
+    if (n_heads < 1 || n_kv_heads < 1 || n_heads % n_kv_heads) return 0;
+    const int32_t group = n_heads / n_kv_heads;
+    return kStatusBytes + decode_part_o_bytes(group) + size_t{2} * DECODE_MAX_BLOCKS * decode_rows_per_chunk(group) * sizeof(float);
+}
+
+int32_t hydra_attn_decode(const void* q, int64_t q_stride, const hydra_paged_cache_t* cache, int32_t n_heads, float softmax_scale,
+                          void* out, float* lse, void* workspace, size_t workspace_bytes, void* cuda_stream)
+{
+    if (int32_t s = check_cache(cache)) return s;
+    const hydra_paged_cache_t& c = *cache;
+    if (n_heads < 1 || n_heads % c.n_kv_heads || !(softmax_scale > 0.f) || !std::isfinite(softmax_scale) ||
+        q_stride < int64_t{n_heads} * c.d_qk)
+        return HYDRA_ERR_INVALID_ARG;
+    const int64_t rows = int64_t{c.n_pages} * c.n_kv_heads;
+    if (!kernel_set(c.d_qk, c.d_v) || c.page_size % 8 || rows > INT32_MAX / c.page_size || q_stride % 8 ||
+        int64_t{c.n_seqs} * n_heads > INT32_MAX)
+        return HYDRA_ERR_UNSUPPORTED;
+    if (!workspace || !aligned16(workspace)) return HYDRA_ERR_INVALID_ARG;
+    if (workspace_bytes < hydra_workspace_bytes_decode(n_heads, c.n_kv_heads)) return HYDRA_ERR_WORKSPACE_TOO_SMALL;
+    if (c.n_seqs > 0) {
+        if (int32_t s = check_cache_pointers(cache)) return s;
+        if (!q || !out || !lse || !aligned16(q) || !aligned16(out) || !aligned16(lse)) return HYDRA_ERR_INVALID_ARG;
+    }
+    int sms = 0;
+    if (int32_t s = device_info(&sms)) return s;
+    if (c.n_seqs == 0) return HYDRA_OK;
+    cudaStream_t stream = static_cast<cudaStream_t>(cuda_stream);
+    // the status block, as in the forward: marked with the call's number, or cleared where the launches are recorded
+    cudaStreamCaptureStatus capturing = cudaStreamCaptureStatusNone;
+    if (cudaStreamIsCapturing(stream, &capturing) != cudaSuccess) return HYDRA_ERR_CUDA;
+    uint64_t call_tag = 0;
+    if (capturing == cudaStreamCaptureStatusNone) call_tag = next_call_tag();
+    else if (launch_reset(static_cast<StatusBlock*>(workspace), false, stream) != cudaSuccess) return HYDRA_ERR_CUDA;
+    DecodeParams p{};
+    p.q = static_cast<const uint16_t*>(q);
+    p.q_stride = q_stride;
+    p.page_table = c.page_table;
+    p.seq_lens = c.seq_lens;
+    p.out = static_cast<uint16_t*>(out);
+    p.lse = lse;
+    p.h = n_heads;
+    p.kv_heads = c.n_kv_heads;
+    p.group = n_heads / c.n_kv_heads;
+    const int32_t per_chunk = decode_rows_per_chunk(p.group);
+    p.chunks = (p.group + per_chunk - 1) / per_chunk;
+    uint8_t* const ws = static_cast<uint8_t*>(workspace);
+    p.part_o = reinterpret_cast<float*>(ws + kStatusBytes);
+    p.part_lse2 = reinterpret_cast<float*>(ws + kStatusBytes + decode_part_o_bytes(p.group));
+    p.n_seqs = c.n_seqs;
+    p.max_pages = c.max_pages;
+    p.page_size = c.page_size;
+    p.n_pages = c.n_pages;
+    p.max_len = static_cast<int32_t>(std::min<int64_t>(int64_t{c.max_pages} * c.page_size, INT32_MAX - DECODE_KEYS));
+    p.box_rows = c.page_size % 16 ? 8 : 16;
+    p.scale_log2 = softmax_scale * 1.4426950408889634f;
+    p.status = static_cast<StatusBlock*>(workspace);
+    p.wait_limit_ns = g_wait_limit_ns.load();
+    p.debug_stall_ns = g_debug_stall_ns[HYDRA_STALL_DECODE].load();
+    CUtensorMap mk, mv;
+    if (make_rows_map(&mk, c.k, rows * c.page_size, c.d_qk, p.box_rows) || make_rows_map(&mv, c.v, rows * c.page_size, c.d_v, p.box_rows))
+        return HYDRA_ERR_CUDA;
+    const int grid = std::min(sms, DECODE_MAX_BLOCKS);
+    {
+        ScopedKernelTimer timer(K_FWD, stream);
+        if (launch_decode(mk, mv, p, c.d_qk, call_tag, grid, stream) != cudaSuccess) return HYDRA_ERR_CUDA;
+        g_launches += 1;
+    }
+    ScopedKernelTimer timer(K_MERGE, stream);
+    if (launch_decode_join(p, grid, stream) != cudaSuccess) return HYDRA_ERR_CUDA;
     g_launches += 1;
     return HYDRA_OK;
 }

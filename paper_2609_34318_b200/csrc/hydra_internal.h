@@ -14,6 +14,8 @@ constexpr int D_V = HYDRA_D_V;
 constexpr int TILE = 128;       // rows of a q tile and of a kv tile
 constexpr int SUB = 64;         // rows of a q sub-tile in the key-side backward kernel
 constexpr int FWD_SHORT_KEYS = 64;   // keys per step of the short-sequence forward kernel
+constexpr int DECODE_KEYS = 64;      // keys of a tile of the attention over a paged cache
+constexpr int DECODE_MAX_BLOCKS = 148;
 
 // One (q-chunk, kv-chunk) pair with absolute token offsets, as the kernels see it.
 struct PairDev {
@@ -293,6 +295,26 @@ struct MergeParams {
     int32_t split;              // thread blocks that share an item (set by launch_merge)
 };
 
+struct DecodeParams {
+    const uint16_t* q;          // bf16 [n_seqs, h, d_qk], rows of a sequence q_stride elements apart
+    int64_t q_stride;
+    const int32_t* page_table;  // [n_seqs, max_pages]
+    const int32_t* seq_lens;    // [n_seqs]
+    uint16_t* out; float* lse;  // bf16 [n_seqs, h, d_v]; [h, n_seqs]
+    // (O, log2 of the sum of 2^score) of pairs cut between thread blocks: two slots per block, a row per query head
+    float* part_o; float* part_lse2;
+    int32_t n_seqs, max_pages, page_size, n_pages;
+    int32_t max_len;            // tokens that a row of the page table holds
+    int32_t box_rows;           // rows of a TMA box: a divisor of page_size
+    int32_t h, kv_heads;
+    int32_t group;              // query heads per K / V head
+    int32_t chunks;             // thread blocks' shares of a group (decode_rows_per_chunk query heads each)
+    float scale_log2;           // softmax_scale * log2(e)
+    StatusBlock* status;
+    uint64_t wait_limit_ns;
+    uint64_t debug_stall_ns;    // test hook (hydra_debug_stall): 0 in normal operation
+};
+
 // The tensor-core kernels exist once per supported q / k head dimension (the kernel files are compiled
 // twice): the unsuffixed set for d_qk = 192, the _d128 set for d_qk = 128; d_v = 128 in both.
 #define HYDRA_DECLARE_KERNEL_SET(SUFFIX)                                                                              \
@@ -339,6 +361,18 @@ cudaError_t launch_mla_kv_assemble_bwd(const void* dk, const void* dv, const int
 cudaError_t launch_gate(const void* out, const void* gate, void* y, int64_t n8, cudaStream_t stream);
 cudaError_t launch_gate_bwd(const void* dy, const void* out, const void* gate, void* d_out, void* d_gate, int64_t n8,
                             cudaStream_t stream);
+// attention of one new token over a paged cache, and the join of what thread blocks had of one pair (decode_kernel.cu)
+int32_t decode_rows_per_chunk(int32_t group);
+cudaError_t launch_decode(const CUtensorMap& mk, const CUtensorMap& mv, const DecodeParams& p, int32_t d_qk, uint64_t call_tag,
+                          int grid, cudaStream_t stream);
+cudaError_t launch_decode_join(const DecodeParams& p, int decode_grid, cudaStream_t stream);
+// rotary positions with several axes; new keys and values into a paged cache (pe: MLA form, k is the up-projection)
+// (paged_ops.cu)
+cudaError_t launch_rope_axes(const void* x, int64_t x_stride, const int32_t* positions, int64_t n_tokens, int32_t n_heads,
+                             int32_t head_dim, const hydra_rope_t& rope, int inverse, void* y, int64_t y_stride, cudaStream_t stream);
+cudaError_t launch_kv_append(const void* k, int64_t k_stride, const void* v, int64_t v_stride, const void* pe, int64_t pe_stride,
+                             const int32_t* positions, const int32_t* cu_new, int64_t n_tokens, const hydra_rope_t* rope,
+                             const hydra_paged_cache_t& cache, cudaStream_t stream);
 // clears the status block (of which keep_status leaves all but the work-queue heads)
 cudaError_t launch_reset(StatusBlock* status, bool keep_status, cudaStream_t stream);
 // D = rowsum(dO * O); also clears the status block and `zero_bytes` (a multiple of 16) at `zero`

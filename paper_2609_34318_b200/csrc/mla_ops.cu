@@ -6,31 +6,16 @@
 // the readings taken (rotary pairs (2i, 2i+1), angle = position * theta^(-2i/rope_dim); one rotary key
 // vector per token shared by all heads; up-projection rows laid out [key part | value]; gate = sigmoid)
 // are stated with each entry point in the header.
-#include <cuda_bf16.h>
-
 #include <algorithm>
-#include <initializer_list>
-
 #include <cmath>
 
-#include "hydra_internal.h"
-#include "sm100_ptx.cuh"
+#include "elementwise.cuh"
 
 namespace hydra {
 namespace {
 
 constexpr int kRopeThreads = 128;
 constexpr int kMaxRopePairs = 128;          // rotary dimensions up to 256
-
-__device__ __forceinline__ float2 bf2_to_f2(uint32_t w)
-{
-    return make_float2(__uint_as_float(w << 16), __uint_as_float(w & 0xffff0000u));
-}
-__device__ __forceinline__ uint32_t f2_to_bf2(float lo, float hi)
-{
-    const __nv_bfloat162 h = __floats2bfloat162_rn(lo, hi);
-    return *reinterpret_cast<const uint32_t*>(&h);
-}
 
 // cos / sin of position * theta^(-2i/rope_dim), i < rope_dim / 2, for one token, into shared memory. The
 // angle is formed and reduced modulo 2 pi in double precision: at position 262143 a single-precision
@@ -160,56 +145,6 @@ hydra_mla_kv_assemble_bwd_kernel(const uint32_t* __restrict__ dk, const uint32_t
     overlap_next_launch();
 }
 
-inline bool aligned16_all(std::initializer_list<const void*> ptrs)
-{
-    uintptr_t bits = 0;
-    for (const void* p : ptrs) bits |= reinterpret_cast<uintptr_t>(p);
-    return (bits & 15u) == 0;
-}
-
-// kWords 32-bit words (pairs of bf16) per thread and access: 4 (16 bytes), or 8 (32 bytes) where the element
-// count and the buffers allow it. Half as many threads then share the loop and address arithmetic.
-template <int kWords>
-struct Words { uint32_t w[kWords]; };
-template <int kWords>
-__device__ __forceinline__ Words<kWords> ld_words(const void* base, int64_t i)
-{
-    Words<kWords> v;
-    if constexpr (kWords == 8) {
-        const Words<8>* p = static_cast<const Words<8>*>(base) + i;
-        asm volatile("ld.global.nc.L1::no_allocate.v8.u32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
-                     : "=r"(v.w[0]), "=r"(v.w[1]), "=r"(v.w[2]), "=r"(v.w[3]), "=r"(v.w[4]), "=r"(v.w[5]),
-                       "=r"(v.w[6]), "=r"(v.w[7])
-                     : "l"(p));
-    } else {
-        const uint4 t = static_cast<const uint4*>(base)[i];
-        v.w[0] = t.x; v.w[1] = t.y; v.w[2] = t.z; v.w[3] = t.w;
-    }
-    return v;
-}
-// the same from memory that this kernel writes
-template <int kWords>
-__device__ __forceinline__ Words<kWords> ld_words_coherent(const void* base, int64_t i)
-{
-    Words<kWords> v;
-    const uint4* p = reinterpret_cast<const uint4*>(static_cast<const Words<kWords>*>(base) + i);
-#pragma unroll
-    for (int j = 0; j < kWords / 4; ++j) {
-        const uint4 t = p[j];
-        v.w[4 * j] = t.x; v.w[4 * j + 1] = t.y; v.w[4 * j + 2] = t.z; v.w[4 * j + 3] = t.w;
-    }
-    return v;
-}
-template <int kWords>
-__device__ __forceinline__ void st_words(void* base, int64_t i, const Words<kWords>& v)
-{
-    if constexpr (kWords == 8) {
-        st_global_v8(static_cast<Words<8>*>(base) + i, v.w);
-    } else {
-        static_cast<uint4*>(base)[i] = make_uint4(v.w[0], v.w[1], v.w[2], v.w[3]);
-    }
-}
-
 // ---------------------------------------------------------------------------------------------
 // Vector forms of the three kernels above (kWords rotary pairs, 16 or 32 bytes, per access), used when the head
 // dimensions are multiples of the vector and the buffers aligned to it. All three are bound by memory, and what keeps
@@ -221,25 +156,9 @@ __device__ __forceinline__ void st_words(void* base, int64_t i, const Words<kWor
 // 155 -> 99.3 (6.1); 16384 tokens, 8 heads 20.8 -> 20.5, 31.3 -> 26.8 and 41.2 -> 31.3; 100 tokens, 128 heads 6.7 -> 5.7,
 // 9.7 -> 6.4 and 20.1 -> 6.1. A copy of as many bytes runs at 6.3 TB/s.
 // ---------------------------------------------------------------------------------------------
-constexpr int kVecThreads = 256;
 // Vectors of a thread in flight. The assembly gains from four (two: 100 us instead of 97.3); the other two need their registers
 // for more blocks (rotary embedding with four, two, one: 71.5, 66.6, 68.3 us; assembly backward 113, 99.3, 104).
 constexpr int kAsmUnroll = 4, kRopeUnroll = 2, kAsmBwdUnroll = 2;
-
-// n / d for n * d < 2^32 (`fits` below): the error of n * m / 2^32, m = floor(2^32 / d) + 1, is under 1 / d
-struct Div {
-    uint32_t d, m;
-    explicit Div(uint32_t div) : d(div), m(div > 1 ? static_cast<uint32_t>((uint64_t{1} << 32) / div) + 1 : 0) {}
-    __device__ __forceinline__ uint32_t operator()(uint32_t n) const { return m ? __umulhi(n, m) : n; }
-};
-
-// cos / sin of position * freq, the angle reduced as in rope_table
-__device__ __forceinline__ void rope_angle(int32_t pos, double freq, float& cs, float& sn)
-{
-    double ang = static_cast<double>(pos) * freq;
-    ang -= 6.283185307179586476925 * floor(ang / 6.283185307179586476925);
-    sincosf(static_cast<float>(ang), &sn, &cs);
-}
 
 // A block takes `per_item` tokens at once; thread (token of the item) * pairs + pair forms that pair's angle.
 struct VecItems {
@@ -268,34 +187,6 @@ struct VecItems {
         return static_cast<int>(std::min<int64_t>(items, 148 * 32));
     }
 };
-
-template <int kWords>
-__device__ __forceinline__ Words<kWords> rotate_vec(const Words<kWords>& w, const float* cp, const float* sp)
-{
-    Words<kWords> out;
-#pragma unroll
-    for (int j = 0; j < kWords; ++j) {
-        const float2 v = bf2_to_f2(w.w[j]);
-        out.w[j] = f2_to_bf2(v.x * cp[j] - v.y * sp[j], v.x * sp[j] + v.y * cp[j]);
-    }
-    return out;
-}
-
-// n vectors of a block: load(e) gives vector e and where it goes, store(at, v) puts it there
-template <int kWords, int kVecUnroll, class Load, class Store>
-__device__ __forceinline__ void move_vecs(uint32_t n, Load load, Store store)
-{
-    for (uint32_t e0 = threadIdx.x; e0 < n; e0 += kVecUnroll * kVecThreads) {
-        Words<kWords> v[kVecUnroll];
-        uint32_t at[kVecUnroll];
-#pragma unroll
-        for (int u = 0; u < kVecUnroll; ++u)
-            if (e0 + u * kVecThreads < n) v[u] = load(e0 + u * kVecThreads, at[u]);
-#pragma unroll
-        for (int u = 0; u < kVecUnroll; ++u)
-            if (e0 + u * kVecThreads < n) store(at[u], v[u]);
-    }
-}
 
 // the rotary vectors and the others in loops of their own: no lane waits for a rotation it does not do. In place (x == y)
 // only the rotary columns move.
@@ -510,13 +401,6 @@ hydra_gate_bwd_kernel(const void* __restrict__ dy, const void* __restrict__ out,
     overlap_next_launch();
 }
 
-inline bool all_aligned32(std::initializer_list<const void*> ptrs)
-{
-    uintptr_t bits = 0;
-    for (const void* p : ptrs) bits |= reinterpret_cast<uintptr_t>(p);
-    return (bits & 31u) == 0;
-}
-
 int grid_for(int64_t work_items, int per_block)
 {
     const int64_t blocks = (work_items + per_block - 1) / per_block;
@@ -524,15 +408,6 @@ int grid_for(int64_t work_items, int per_block)
 }
 
 }  // namespace
-
-// kWords of the vector kernels that the dimensions and buffers admit: 8, 4 or 0 (the four-byte kernels)
-static int words_for(std::initializer_list<int32_t> dims, std::initializer_list<const void*> ptrs)
-{
-    int32_t bits = 0;
-    for (int32_t d : dims) bits |= d;
-    if (bits % 16 == 0 && all_aligned32(ptrs)) return 8;
-    return bits % 8 == 0 && aligned16_all(ptrs) ? 4 : 0;
-}
 
 template <int kWords>
 static cudaError_t launch_rope_vec(const VecItems& it, const uint32_t* x, const int32_t* positions, uint32_t* y, int32_t head_dim,
