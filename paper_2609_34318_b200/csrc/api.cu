@@ -2936,10 +2936,8 @@ int32_t make_rows_map(CUtensorMap* map, const void* base, int64_t n_rows, int32_
     return r == CUDA_SUCCESS ? HYDRA_OK : HYDRA_ERR_CUDA;
 }
 
-size_t decode_part_o_bytes(int32_t group)
-{
-    return size_t{2} * DECODE_MAX_BLOCKS * decode_rows_per_chunk(group) * D_V * sizeof(float);
-}
+// partial results: two slots per thread block, up to 32 query heads (8 or 16 if a group has no more)
+size_t decode_slot_rows(int32_t group) { return size_t{2} * DECODE_MAX_BLOCKS * (group <= 8 ? 8 : group <= 16 ? 16 : 32); }
 }  // namespace
 
 int32_t hydra_rope_axes(const void* x, int64_t x_stride, const int32_t* positions, int64_t n_tokens, int32_t n_heads,
@@ -2990,7 +2988,7 @@ size_t hydra_workspace_bytes_decode(int32_t n_heads, int32_t n_kv_heads)
 {
     if (n_heads < 1 || n_kv_heads < 1 || n_heads % n_kv_heads) return 0;
     const int32_t group = n_heads / n_kv_heads;
-    return kStatusBytes + decode_part_o_bytes(group) + size_t{2} * DECODE_MAX_BLOCKS * decode_rows_per_chunk(group) * sizeof(float);
+    return kStatusBytes + decode_slot_rows(group) * (D_V + 1) * sizeof(float);
 }
 
 int32_t hydra_attn_decode(const void* q, int64_t q_stride, const hydra_paged_cache_t* cache, int32_t n_heads, float softmax_scale,
@@ -3031,16 +3029,18 @@ int32_t hydra_attn_decode(const void* q, int64_t q_stride, const hydra_paged_cac
     p.h = n_heads;
     p.kv_heads = c.n_kv_heads;
     p.group = n_heads / c.n_kv_heads;
-    const int32_t per_chunk = decode_rows_per_chunk(p.group);
-    p.chunks = (p.group + per_chunk - 1) / per_chunk;
+    const DecodeForm form = decode_form(c.d_qk, p.group);
+    p.chunk_rows = form.chunk_rows;
+    p.chunks = (p.group + form.chunk_rows - 1) / form.chunk_rows;
+    p.tile_keys = form.tile_keys;
     uint8_t* const ws = static_cast<uint8_t*>(workspace);
     p.part_o = reinterpret_cast<float*>(ws + kStatusBytes);
-    p.part_lse2 = reinterpret_cast<float*>(ws + kStatusBytes + decode_part_o_bytes(p.group));
+    p.part_lse2 = p.part_o + decode_slot_rows(p.group) * D_V;
     p.n_seqs = c.n_seqs;
     p.max_pages = c.max_pages;
     p.page_size = c.page_size;
     p.n_pages = c.n_pages;
-    p.max_len = static_cast<int32_t>(std::min<int64_t>(int64_t{c.max_pages} * c.page_size, INT32_MAX - DECODE_KEYS));
+    p.max_len = static_cast<int32_t>(std::min<int64_t>(int64_t{c.max_pages} * c.page_size, INT32_MAX - 64));
     p.box_rows = c.page_size % 16 ? 8 : 16;
     p.scale_log2 = softmax_scale * 1.4426950408889634f;
     p.status = static_cast<StatusBlock*>(workspace);
@@ -3049,7 +3049,7 @@ int32_t hydra_attn_decode(const void* q, int64_t q_stride, const hydra_paged_cac
     CUtensorMap mk, mv;
     if (make_rows_map(&mk, c.k, rows * c.page_size, c.d_qk, p.box_rows) || make_rows_map(&mv, c.v, rows * c.page_size, c.d_v, p.box_rows))
         return HYDRA_ERR_CUDA;
-    const int grid = std::min(sms, DECODE_MAX_BLOCKS);
+    const int grid = std::min(sms * form.per_sm, DECODE_MAX_BLOCKS);
     {
         ScopedKernelTimer timer(K_FWD, stream);
         if (launch_decode(mk, mv, p, c.d_qk, call_tag, grid, stream) != cudaSuccess) return HYDRA_ERR_CUDA;

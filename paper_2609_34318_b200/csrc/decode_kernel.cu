@@ -26,9 +26,7 @@
 namespace hydra {
 namespace {
 
-constexpr int kKeys = DECODE_KEYS;          // keys of a tile
-constexpr int kKeyWarps = 4;                // warps that share a tile's keys, 16 each
-constexpr int kSmemLimit = 227 * 1024;
+constexpr int kSmemOfSm = 228 * 1024;        // of which the system takes 1 KB per thread block
 constexpr float kRaise = 8.f;               // the running maximum is raised when it grew by more than 2^8
 
 enum : int32_t { FLAG_FIRST = 1, FLAG_LAST = 2, FLAG_END = 4, FLAG_PARTIAL = 8, FLAG_SECOND_SLOT = 16 };
@@ -38,22 +36,25 @@ struct __align__(16) StageDesc {
     int32_t flags;
 };
 
-// kMTiles: 16-row tiles of query heads per thread block
-template <int kDqk, int kMTiles>
+// Thread blocks of one kind. kNTiles: tiles of eight query heads per warp; kHeadWarps: warps that share a key's query heads;
+// kKeyWarps: warps that share a tile's keys, 16 each; kPerSm: thread blocks per SM.
+template <int kDqk_, int kNTiles_, int kHeadWarps_, int kKeyWarps_, int kPerSm_>
 struct Shape {
-    static constexpr int kRows = 16 * kMTiles;
-    static constexpr int kConsumers = kKeyWarps * kMTiles;              // warps
+    static constexpr int kDqk = kDqk_, kNTiles = kNTiles_, kHeadWarps = kHeadWarps_, kKeyWarps = kKeyWarps_, kPerSm = kPerSm_;
+    static constexpr int kKeys = 16 * kKeyWarps;                        // of a tile
+    static constexpr int kRows = 8 * kNTiles * kHeadWarps;              // query heads of a block
+    static constexpr int kConsumers = kKeyWarps * kHeadWarps;           // warps
     static constexpr int kThreads = 32 * (kConsumers + 1);
     static constexpr int kKBytes = kKeys * kDqk * 2, kVBytes = kKeys * D_V * 2, kQBytes = kRows * kDqk * 2;
     static constexpr int kStage = kKBytes + kVBytes + kQBytes;
-    // floats between rows of the join buffer: 8 more than a row keep the banks of a warp's rows apart, 4 more in pairs
-    static constexpr int kJoinStride = D_V + (kMTiles == 1 ? 8 : 4);
+    // floats between rows of the join buffer: 2 * 132 = 8 (mod 32), the eight values and four heads of a warp's store meet 32 banks
+    static constexpr int kJoinStride = D_V + 4;
     static constexpr int kJoin = kKeyWarps * kRows * kJoinStride * 4;
-    static constexpr int kFixed = 1024 + 2560;                          // alignment of the ring; barriers, descriptors, (m, l)
-    static constexpr int kFit = (kSmemLimit - kJoin - kFixed) / kStage;
-    static constexpr int kStages = kFit < 6 ? kFit : 6;
+    static constexpr int kFixed = 1024 + 512 + 16 * kKeyWarps * kRows;      // alignment of the ring; barriers and descriptors; (m, l)
+    static constexpr int kFit = (kSmemOfSm / kPerSm - 1024 - kJoin - kFixed) / kStage;
+    static constexpr int kStages = kFit < 8 ? kFit : 8;
     static constexpr int kSmem = kStages * kStage + kJoin + 1024;
-    static_assert(kStage % 1024 == 0 && kStages >= 3, "ring");
+    static_assert(kStage % 1024 == 0 && kStages >= 2, "ring");
 };
 
 __device__ __forceinline__ void ldmatrix_x4(uint32_t addr, uint32_t (&r)[4])
@@ -65,6 +66,13 @@ __device__ __forceinline__ void ldmatrix_x4_trans(uint32_t addr, uint32_t (&r)[4
 {
     asm volatile("ldmatrix.sync.aligned.m8n8.x4.trans.shared.b16 {%0, %1, %2, %3}, [%4];"
                  : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(addr) : "memory");
+}
+// an 8 x 8 matrix of 16-bit values, a thread's two of row lane / 4, becomes its transpose
+__device__ __forceinline__ uint32_t transpose_8x8(uint32_t x)
+{
+    uint32_t y;
+    asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(y) : "r"(x));
+    return y;
 }
 // c[16 x 8] += a[16 x 16] b[16 x 8]
 __device__ __forceinline__ void mma_bf16(float (&c)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1)
@@ -81,7 +89,7 @@ __device__ __forceinline__ int32_t seq_len_of(const DecodeParams& p, int32_t b)
 {
     return min(max(__ldcg(p.seq_lens + b), 0), p.max_len);
 }
-__device__ __forceinline__ int32_t tiles_of(int32_t len) { return (len + kKeys - 1) / kKeys; }
+__device__ __forceinline__ int32_t tiles_of(const DecodeParams& p, int32_t len) { return (len + p.tile_keys - 1) / p.tile_keys; }
 
 // The run of thread block c of n: tiles [total c / n, total (c + 1) / n); the block that has tile t.
 __device__ __forceinline__ int64_t run_start(int64_t total, int64_t c, int64_t n) { return total * c / n; }
@@ -89,13 +97,12 @@ __device__ __forceinline__ int64_t block_of(int64_t total, int64_t t, int64_t n)
 
 struct Start { int32_t seq; int32_t pad; int64_t before; int64_t total; };
 
-// kRow8: no more than eight rows of a tile are query heads, the lower half of every product's rows is padding
-template <int kDqk, int kMTiles, bool kRow8>
-__global__ void __launch_bounds__(Shape<kDqk, kMTiles>::kThreads, 1)
+template <class S>
+__global__ void __launch_bounds__(S::kThreads, S::kPerSm)
 hydra_decode_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_v, const DecodeParams p,
                     const uint64_t call_tag)
 {
-    using S = Shape<kDqk, kMTiles>;
+    constexpr int kDqk = S::kDqk, kKeys = S::kKeys, kKeyWarps = S::kKeyWarps, kNT = S::kNTiles;
     constexpr int kBoxesK = kDqk / 64, kBoxesV = D_V / 64, kBox = kKeys * 128;      // 64 columns of a tile
     extern __shared__ uint8_t smem_raw[];
     __shared__ __align__(8) uint64_t bars[2 * S::kStages + 2];
@@ -134,7 +141,7 @@ hydra_decode_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_cons
         const int per = (p.n_seqs + S::kThreads - 1) / S::kThreads;
         const int b0 = min(tid * per, p.n_seqs), b1 = min(b0 + per, p.n_seqs);
         int64_t mine = 0;
-        for (int b = b0; b < b1; ++b) mine += tiles_of(seq_len_of(p, b));
+        for (int b = b0; b < b1; ++b) mine += tiles_of(p, seq_len_of(p, b));
         int64_t sum = mine;
 #pragma unroll
         for (int d = 1; d < 32; d *= 2) {
@@ -156,7 +163,7 @@ hydra_decode_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_cons
             int64_t at = before;
             int b = b0;
             for (;; ++b) {
-                const int n = tiles_of(seq_len_of(p, b));
+                const int n = tiles_of(p, seq_len_of(p, b));
                 if (first < at + n) break;
                 at += n;
             }
@@ -178,7 +185,7 @@ hydra_decode_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_cons
         } else {
             const int32_t boxes = kKeys / p.box_rows;   // of a tile; lane j asks for box j's page
             const int32_t key_in_tile = lane * p.box_rows;
-            int32_t b = s_start.seq, len = seq_len_of(p, b), n_tiles = tiles_of(len);
+            int32_t b = s_start.seq, len = seq_len_of(p, b), n_tiles = tiles_of(p, len);
             int64_t base = s_start.before * per_seq;    // first tile of sequence b
             int32_t in_seq = static_cast<int32_t>((lo - base) / n_tiles);           // pair of the sequence, and tile of the pair
             int32_t tile = static_cast<int32_t>((lo - base) - static_cast<int64_t>(in_seq) * n_tiles);
@@ -237,7 +244,7 @@ hydra_decode_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_cons
                         in_seq = 0;
                         if (t + 1 < hi) {
                             do { len = seq_len_of(p, ++b); } while (len == 0);
-                            n_tiles = tiles_of(len);
+                            n_tiles = tiles_of(p, len);
                         }
                     }
                 }
@@ -246,12 +253,14 @@ hydra_decode_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_cons
         }
     } else {
         // ------------------------------------------------------------------ scores, softmax, O
-        const int kw = warp % kKeyWarps, mt = warp / kKeyWarps;
-        uint32_t q[kDqk / 16][4];
-        float o[D_V / 8][4];
-        float m[2], l[2];
-        const uint32_t k_row = static_cast<uint32_t>(kw * 16 + (lane & 7) + ((lane >> 4) & 1) * 8), k_unit = (lane >> 3) & 1;
-        const uint32_t v_row = static_cast<uint32_t>(kw * 16 + (lane & 15)), v_unit = (lane >> 4) & 1;
+        // Keys stand on the 16 rows of a product and query heads on its 8 columns: S^T = K Q^T, O^T = V^T P^T. A thread has the
+        // heads 2 (lane mod 4) and the one after it, of every tile of eight, and of a product the rows lane / 4 and 8 more.
+        const int kw = warp % kKeyWarps, head_of_warp = warp / kKeyWarps * 8 * kNT, key_of_lane = lane >> 2;
+        uint32_t q[kDqk / 16][kNT][2];
+        float o[D_V / 16][kNT][4];
+        float m[kNT][2], l[kNT][2];
+        const uint32_t k_row = static_cast<uint32_t>(kw * 16 + (lane & 15)), k_unit = (lane >> 4) & 1;
+        const uint32_t v_row = static_cast<uint32_t>(kw * 16 + (lane & 7) + ((lane >> 4) & 1) * 8), v_unit = (lane >> 3) & 1;
         uint32_t joins = 0;
         for (uint32_t n = 0;; ++n) {
             const int st = static_cast<int>(n % S::kStages);
@@ -260,108 +269,132 @@ hydra_decode_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_cons
             if (d.flags & FLAG_END) break;
             const uint32_t stage = ring + static_cast<uint32_t>(st) * S::kStage;
             if (d.flags & FLAG_FIRST) {
-                const uint32_t q_at = stage + S::kKBytes + S::kVBytes + static_cast<uint32_t>(mt * 16 + (lane & 15)) * (kDqk * 2) + (lane >> 4) * 16;
 #pragma unroll
-                for (int ks = 0; ks < kDqk / 16; ++ks) ldmatrix_x4(q_at + ks * 32, q[ks]);
+                for (int t = 0; t < kNT; ++t) {
+                    const uint32_t q_at = stage + S::kKBytes + S::kVBytes + static_cast<uint32_t>(head_of_warp + t * 8 + (lane & 7)) * (kDqk * 2) + (lane >> 3) * 16;
 #pragma unroll
-                for (int j = 0; j < D_V / 8; ++j)
+                    for (int ks = 0; ks < kDqk / 16; ks += 2) {
+                        uint32_t f[4];
+                        ldmatrix_x4(q_at + ks * 32, f);
+                        q[ks][t][0] = f[0]; q[ks][t][1] = f[1]; q[ks + 1][t][0] = f[2]; q[ks + 1][t][1] = f[3];
+                    }
+                }
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) o[j][e] = 0.f;
-                m[0] = m[1] = neg_inf();
-                l[0] = l[1] = 0.f;
+                for (int i = 0; i < D_V / 16 * kNT * 4; ++i) o[i / (4 * kNT)][i / 4 % kNT][i % 4] = 0.f;
+#pragma unroll
+                for (int t = 0; t < kNT; ++t) {
+                    m[t][0] = m[t][1] = neg_inf();
+                    l[t][0] = l[t][1] = 0.f;
+                }
             }
             const uint32_t seen = static_cast<uint32_t>(d.seen >> (kw * 16)) & 0xffffu;
             if (seen) {
-                float s[2][2][4];                       // [even / odd k step][keys 0-7 / 8-15]: four chains of products
+                float s[2][kNT][4];                     // even and odd steps: two chains of products per tile of heads
 #pragma unroll
-                for (int i = 0; i < 16; ++i) s[i >> 3][(i >> 2) & 1][i & 3] = 0.f;
+                for (int i = 0; i < 8 * kNT; ++i) s[i / (4 * kNT)][i / 4 % kNT][i % 4] = 0.f;
 #pragma unroll
                 for (int ks = 0; ks < kDqk / 16; ++ks) {
                     uint32_t kf[4];
                     ldmatrix_x4(stage + (ks / 4) * kBox + k_row * 128 + ((((ks % 4) * 2 + k_unit) ^ (k_row & 7)) << 4), kf);
-                    mma_bf16(s[ks & 1][0], q[ks], kf[0], kf[1]);
-                    mma_bf16(s[ks & 1][1], q[ks], kf[2], kf[3]);
-                }
-                const uint32_t bits = seen >> (2 * (lane & 3));     // of keys +0, +1, +8, +9
-                uint32_t ph[4], pl[4];
 #pragma unroll
-                for (int r = 0; r < (kRow8 ? 1 : 2); ++r) {
-                    float x[4];
+                    for (int t = 0; t < kNT; ++t) mma_bf16(s[ks & 1][t], kf, q[ks][t][0], q[ks][t][1]);
+                }
+                const uint32_t bits = seen >> key_of_lane;      // bit 0: this thread's first key, bit 8: its second
+                uint32_t ph[kNT][2], pl[kNT][2];
+#pragma unroll
+                for (int t = 0; t < kNT; ++t) {
+                    float x[4];                         // [key][head]
 #pragma unroll
                     for (int e = 0; e < 4; ++e) {
-                        x[e] = (s[0][e >> 1][2 * r + (e & 1)] + s[1][e >> 1][2 * r + (e & 1)]) * p.scale_log2;
-                        if (!(bits >> ((e & 1) + (e >> 1) * 8) & 1u)) x[e] = neg_inf();
+                        x[e] = (s[0][t][e] + s[1][t][e]) * p.scale_log2;
+                        if (!(bits >> (8 * (e >> 1)) & 1u)) x[e] = neg_inf();
                     }
-                    float top = fmaxf(fmaxf(x[0], x[1]), fmaxf(x[2], x[3]));
-                    top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 1));
-                    top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 2));
-                    const bool raise = top > m[r] + kRaise;
-                    if (__any_sync(0xffffffffu, raise)) {
-                        const float to = raise ? top : m[r], f = raise ? ex2_approx(m[r] - to) : 1.f;
-                        m[r] = to;
-                        l[r] *= f;
+                    // The reference of the exponentials is raised when a score is more than 2^8 above it: until then, no warp-wide
+                    // maximum is needed, one vote says so.
+                    const float top0 = fmaxf(x[0], x[2]), top1 = fmaxf(x[1], x[3]);
+                    if (__any_sync(0xffffffffu, top0 > m[t][0] + kRaise || top1 > m[t][1] + kRaise)) {
 #pragma unroll
-                        for (int j = 0; j < D_V / 8; ++j) { o[j][2 * r] *= f; o[j][2 * r + 1] *= f; }
+                        for (int c = 0; c < 2; ++c) {
+                            float top = c ? top1 : top0;
+#pragma unroll
+                            for (int g = 4; g < 32; g *= 2) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, g));
+                            if (top > m[t][c] + kRaise) {
+                                const float f = ex2_approx(m[t][c] - top);
+                                m[t][c] = top;
+                                l[t][c] *= f;
+#pragma unroll
+                                for (int j = 0; j < D_V / 16; ++j) { o[j][t][c] *= f; o[j][t][c + 2] *= f; }
+                            }
+                        }
                     }
-                    const float ref = m[r] == neg_inf() ? 0.f : m[r];
+                    const float ref0 = m[t][0] == neg_inf() ? 0.f : m[t][0], ref1 = m[t][1] == neg_inf() ? 0.f : m[t][1];
                     float pr[4];
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) pr[e] = ex2_approx(x[e] - ref);
-                    l[r] += (pr[0] + pr[1]) + (pr[2] + pr[3]);
+                    for (int e = 0; e < 4; ++e) pr[e] = ex2_approx(x[e] - (e & 1 ? ref1 : ref0));
+                    l[t][0] += pr[0] + pr[2];
+                    l[t][1] += pr[1] + pr[3];
                     // P as the sum of two bf16 (2^-17 of it is lost): the tensor cores have time for a second product, and with
                     // one the rounding of P alone is as large as that of the bf16 result
 #pragma unroll
                     for (int e = 0; e < 2; ++e) {
                         const uint32_t h = pack_bf16x2(pr[2 * e], pr[2 * e + 1]);
-                        ph[2 * e + r] = h;
-                        pl[2 * e + r] = pack_bf16x2(pr[2 * e] - __uint_as_float(h << 16), pr[2 * e + 1] - __uint_as_float(h & 0xffff0000u));
+                        ph[t][e] = transpose_8x8(h);
+                        pl[t][e] = transpose_8x8(pack_bf16x2(pr[2 * e] - __uint_as_float(h << 16), pr[2 * e + 1] - __uint_as_float(h & 0xffff0000u)));
                     }
                 }
-                if (kRow8) ph[1] = ph[3] = pl[1] = pl[3] = 0u;
                 // rows behind the end hold anything: 0 * NaN must not reach the sums
-                const uint32_t keep0 = (bits & 1u ? 0xffffu : 0u) | (bits & 2u ? 0xffff0000u : 0u);
-                const uint32_t keep1 = (bits & 0x100u ? 0xffffu : 0u) | (bits & 0x200u ? 0xffff0000u : 0u);
+                const uint32_t v_bits = seen >> (2 * (lane & 3));
+                const uint32_t keep0 = (v_bits & 1u ? 0xffffu : 0u) | (v_bits & 2u ? 0xffff0000u : 0u);
+                const uint32_t keep1 = (v_bits & 0x100u ? 0xffffu : 0u) | (v_bits & 0x200u ? 0xffff0000u : 0u);
 #pragma unroll
                 for (int j = 0; j < D_V / 16; ++j) {
                     uint32_t vf[4];
                     ldmatrix_x4_trans(stage + S::kKBytes + (j / 4) * kBox + v_row * 128 + ((((j % 4) * 2 + v_unit) ^ (v_row & 7)) << 4), vf);
-                    if (seen != 0xffffu) { vf[0] &= keep0; vf[1] &= keep1; vf[2] &= keep0; vf[3] &= keep1; }
-                    mma_bf16(o[2 * j], ph, vf[0], vf[1]);
-                    mma_bf16(o[2 * j + 1], ph, vf[2], vf[3]);
-                    mma_bf16(o[2 * j], pl, vf[0], vf[1]);
-                    mma_bf16(o[2 * j + 1], pl, vf[2], vf[3]);
+                    if (seen != 0xffffu) { vf[0] &= keep0; vf[1] &= keep0; vf[2] &= keep1; vf[3] &= keep1; }
+#pragma unroll
+                    for (int t = 0; t < kNT; ++t) {
+                        mma_bf16(o[j][t], vf, ph[t][0], ph[t][1]);
+                        mma_bf16(o[j][t], vf, pl[t][0], pl[t][1]);
+                    }
                 }
             }
             mbar_arrive_warp(empty(st));
             if (!(d.flags & FLAG_LAST)) continue;
 
             // ---------------------------------------------------------------- the warps' shares of the pair, joined
-            const int r0 = mt * 16 + (lane >> 2);
+            const int32_t chunk = d.item % p.chunks, bh = d.item / p.chunks, b = bh / p.kv_heads, kvh = bh - b * p.kv_heads;
+            const int32_t head0 = kvh * p.group + chunk * S::kRows, q_rows = min(S::kRows, p.group - chunk * S::kRows);
+            auto& ml_of = s_ml[joins & 1u];
 #pragma unroll
-            for (int r = 0; r < (kRow8 ? 1 : 2); ++r) {
-                l[r] += __shfl_xor_sync(0xffffffffu, l[r], 1);
-                l[r] += __shfl_xor_sync(0xffffffffu, l[r], 2);
-                if ((lane & 3) == 0) s_ml[joins & 1u][kw][r0 + 8 * r] = make_float2(m[r], l[r]);
-            }
+            for (int t = 0; t < kNT; ++t)
+#pragma unroll
+                for (int c = 0; c < 2; ++c) {
+#pragma unroll
+                    for (int g = 4; g < 32; g *= 2) l[t][c] += __shfl_xor_sync(0xffffffffu, l[t][c], g);
+                    if (lane < 4) ml_of[kw][head_of_warp + t * 8 + 2 * lane + c] = make_float2(m[t][c], l[t][c]);
+                }
             mbar_arrive_warp(join_bar[0]);
             if (!mbar_wait(join_bar[0], joins & 1u, abort_p, limit)) break;
 #pragma unroll
-            for (int r = 0; r < (kRow8 ? 1 : 2); ++r) {
-                float top = neg_inf();
+            for (int t = 0; t < kNT; ++t)
 #pragma unroll
-                for (int w = 0; w < kKeyWarps; ++w) top = fmaxf(top, s_ml[joins & 1u][w][r0 + 8 * r].x);
-                const float f = m[r] == neg_inf() ? 0.f : ex2_approx(m[r] - top);
-                float* dst = join + (kw * S::kRows + r0 + 8 * r) * S::kJoinStride + 2 * (lane & 3);
+                for (int c = 0; c < 2; ++c) {
+                    const int row = head_of_warp + t * 8 + 2 * (lane & 3) + c;
+                    if (row >= q_rows) continue;
+                    float top = neg_inf();
 #pragma unroll
-                for (int j = 0; j < D_V / 8; ++j)
-                    *reinterpret_cast<float2*>(dst + 8 * j) = make_float2(o[j][2 * r] * f, o[j][2 * r + 1] * f);
-            }
+                    for (int w = 0; w < kKeyWarps; ++w) top = fmaxf(top, ml_of[w][row].x);
+                    const float f = m[t][c] == neg_inf() ? 0.f : ex2_approx(m[t][c] - top);
+                    float* dst = join + (kw * S::kRows + row) * S::kJoinStride + key_of_lane;
+#pragma unroll
+                    for (int j = 0; j < D_V / 16; ++j) {
+                        dst[16 * j] = o[j][t][c] * f;
+                        dst[16 * j + 8] = o[j][t][c + 2] * f;
+                    }
+                }
             mbar_arrive_warp(join_bar[1]);
             if (!mbar_wait(join_bar[1], joins & 1u, abort_p, limit)) break;
-            const auto& ml_of = s_ml[joins & 1u];
             ++joins;
-            const int32_t chunk = d.item % p.chunks, bh = d.item / p.chunks, b = bh / p.kv_heads, kvh = bh - b * p.kv_heads;
-            const int32_t head0 = kvh * p.group + chunk * S::kRows, q_rows = min(S::kRows, p.group - chunk * S::kRows);
             const int64_t slot = 2 * static_cast<int64_t>(blockIdx.x) + (d.flags & FLAG_SECOND_SLOT ? 1 : 0);
             for (int e = warp; e < q_rows; e += S::kConsumers) {
                 float top = neg_inf(), sum = 0.f;
@@ -407,7 +440,7 @@ hydra_decode_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_cons
 constexpr int kJoinThreads = 256;
 template <int kWarps>
 __global__ void __launch_bounds__(kJoinThreads)
-hydra_decode_join_kernel(const DecodeParams p, int32_t rows_per_chunk, int32_t n_blocks_max)
+hydra_decode_join_kernel(const DecodeParams p, int32_t n_blocks_max)
 {
     constexpr int kRowsPerBlock = kJoinThreads / 32 / kWarps;
     __shared__ float4 s_acc[kWarps > 1 ? kWarps : 1][32];
@@ -419,7 +452,7 @@ hydra_decode_join_kernel(const DecodeParams p, int32_t rows_per_chunk, int32_t n
     const int32_t per_seq = p.kv_heads * p.chunks;
     int64_t before = 0, all = 0;
     for (int32_t i = lane; i < p.n_seqs; i += 32) {
-        const int32_t n = tiles_of(seq_len_of(p, i));
+        const int32_t n = tiles_of(p, seq_len_of(p, i));
         all += n;
         if (i < b) before += n;
     }
@@ -428,8 +461,8 @@ hydra_decode_join_kernel(const DecodeParams p, int32_t rows_per_chunk, int32_t n
         all += __shfl_xor_sync(0xffffffffu, all, d);
         before += __shfl_xor_sync(0xffffffffu, before, d);
     }
-    const int32_t n_tiles = tiles_of(seq_len_of(p, b));
-    const int32_t kvh = a / p.group, in_group = a - kvh * p.group, chunk = in_group / rows_per_chunk, r = in_group - chunk * rows_per_chunk;
+    const int32_t n_tiles = tiles_of(p, seq_len_of(p, b));
+    const int32_t kvh = a / p.group, in_group = a - kvh * p.group, chunk = in_group / p.chunk_rows, r = in_group - chunk * p.chunk_rows;
     const int64_t total = all * per_seq, n_blocks = min(static_cast<int64_t>(n_blocks_max), total);
     const int64_t t0 = before * per_seq + static_cast<int64_t>(kvh * p.chunks + chunk) * n_tiles;
     const int64_t c0 = n_tiles ? block_of(total, t0, n_blocks) : 0, c1 = n_tiles ? block_of(total, t0 + n_tiles - 1, n_blocks) : 0;
@@ -446,7 +479,7 @@ hydra_decode_join_kernel(const DecodeParams p, int32_t rows_per_chunk, int32_t n
     }
     const int32_t parts = static_cast<int32_t>(c1 - c0) + 1;
     // part i is the beginning of block c0 + i's run, but the first is the end of its block's
-    auto at = [&](int32_t i) { return (2 * (c0 + i) + (i == 0 ? 1 : 0)) * rows_per_chunk + r; };
+    auto at = [&](int32_t i) { return (2 * (c0 + i) + (i == 0 ? 1 : 0)) * p.chunk_rows + r; };
     float top = neg_inf();
     for (int32_t i = lane; i < parts; i += 32) top = fmaxf(top, __ldcg(p.part_lse2 + at(i)));
 #pragma unroll
@@ -477,42 +510,53 @@ hydra_decode_join_kernel(const DecodeParams p, int32_t rows_per_chunk, int32_t n
     if (lane == 0) *lse = top == neg_inf() ? top : (top + log2f(sum)) * 0.6931471805599453f;
 }
 
-template <int kDqk, int kMTiles, bool kRow8>
+struct Form {
+    int32_t rows, tile_keys, per_sm;
+    cudaError_t (*launch)(const CUtensorMap&, const CUtensorMap&, const DecodeParams&, uint64_t, int, cudaStream_t);
+};
+template <class S>
 cudaError_t launch_one(const CUtensorMap& mk, const CUtensorMap& mv, const DecodeParams& p, uint64_t call_tag, int grid,
                        cudaStream_t stream)
 {
-    using S = Shape<kDqk, kMTiles>;
     static OncePerDevice configured;
-    const auto kernel = hydra_decode_kernel<kDqk, kMTiles, kRow8>;
+    const auto kernel = hydra_decode_kernel<S>;
     if (cudaError_t e = allow_dynamic_smem(kernel, S::kSmem, configured)) return e;
     return launch_overlapped(kernel, grid, S::kThreads, S::kSmem, stream, mk, mv, p, call_tag);
 }
+template <class S>
+constexpr Form form_of() { return {S::kRows, S::kKeys, S::kPerSm, launch_one<S>}; }
+
+// by query heads per K / V head
+template <int kDqk>
+const Form& form_for(int32_t group)
+{
+    static constexpr Form one = form_of<Shape<kDqk, 1, 1, 4, 2>>(), two = form_of<Shape<kDqk, 2, 1, 2, 3>>(),
+                          four = form_of<Shape<kDqk, 2, 2, 4, 1>>();
+    return group <= 8 ? one : group <= 16 ? two : four;
+}
+const Form& form_for(int32_t d_qk, int32_t group) { return d_qk == 192 ? form_for<192>(group) : form_for<128>(group); }
 
 }  // namespace
 
-int32_t decode_rows_per_chunk(int32_t group) { return group <= 16 ? 16 : 32; }
+DecodeForm decode_form(int32_t d_qk, int32_t group)
+{
+    const Form& f = form_for(d_qk, group);
+    return {f.rows, f.tile_keys, f.per_sm};
+}
 
 cudaError_t launch_decode(const CUtensorMap& mk, const CUtensorMap& mv, const DecodeParams& p, int32_t d_qk, uint64_t call_tag,
                           int grid, cudaStream_t stream)
 {
-    if (d_qk == 192) {
-        if (p.group <= 8) return launch_one<192, 1, true>(mk, mv, p, call_tag, grid, stream);
-        if (p.group <= 16) return launch_one<192, 1, false>(mk, mv, p, call_tag, grid, stream);
-        return launch_one<192, 2, false>(mk, mv, p, call_tag, grid, stream);
-    }
-    if (p.group <= 8) return launch_one<128, 1, true>(mk, mv, p, call_tag, grid, stream);
-    if (p.group <= 16) return launch_one<128, 1, false>(mk, mv, p, call_tag, grid, stream);
-    return launch_one<128, 2, false>(mk, mv, p, call_tag, grid, stream);
+    return form_for(d_qk, p.group).launch(mk, mv, p, call_tag, grid, stream);
 }
 
 cudaError_t launch_decode_join(const DecodeParams& p, int grid_of_parts, cudaStream_t stream)
 {
     const int64_t rows = static_cast<int64_t>(p.n_seqs) * p.h;
-    const int32_t per = decode_rows_per_chunk(p.group);
     // few pairs have many parts each: eight warps share a row
     if (static_cast<int64_t>(p.n_seqs) * p.kv_heads * p.chunks < grid_of_parts / 4)
-        return launch_overlapped(hydra_decode_join_kernel<8>, static_cast<int>(rows), kJoinThreads, 0, stream, p, per, grid_of_parts);
-    return launch_overlapped(hydra_decode_join_kernel<1>, static_cast<int>((rows + 7) / 8), kJoinThreads, 0, stream, p, per, grid_of_parts);
+        return launch_overlapped(hydra_decode_join_kernel<8>, static_cast<int>(rows), kJoinThreads, 0, stream, p, grid_of_parts);
+    return launch_overlapped(hydra_decode_join_kernel<1>, static_cast<int>((rows + 7) / 8), kJoinThreads, 0, stream, p, grid_of_parts);
 }
 
 }  // namespace hydra

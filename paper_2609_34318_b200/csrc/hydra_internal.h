@@ -14,8 +14,7 @@ constexpr int D_V = HYDRA_D_V;
 constexpr int TILE = 128;       // rows of a q tile and of a kv tile
 constexpr int SUB = 64;         // rows of a q sub-tile in the key-side backward kernel
 constexpr int FWD_SHORT_KEYS = 64;   // keys per step of the short-sequence forward kernel
-constexpr int DECODE_KEYS = 64;      // keys of a tile of the attention over a paged cache
-constexpr int DECODE_MAX_BLOCKS = 148;
+constexpr int DECODE_MAX_BLOCKS = 4 * 148;   // thread blocks of the attention over a paged cache
 
 // One (q-chunk, kv-chunk) pair with absolute token offsets, as the kernels see it.
 struct PairDev {
@@ -308,7 +307,8 @@ struct DecodeParams {
     int32_t box_rows;           // rows of a TMA box: a divisor of page_size
     int32_t h, kv_heads;
     int32_t group;              // query heads per K / V head
-    int32_t chunks;             // thread blocks' shares of a group (decode_rows_per_chunk query heads each)
+    int32_t chunks, chunk_rows; // thread blocks' shares of a group, chunk_rows query heads each
+    int32_t tile_keys;          // keys of a tile
     float scale_log2;           // softmax_scale * log2(e)
     StatusBlock* status;
     uint64_t wait_limit_ns;
@@ -362,7 +362,10 @@ cudaError_t launch_gate(const void* out, const void* gate, void* y, int64_t n8, 
 cudaError_t launch_gate_bwd(const void* dy, const void* out, const void* gate, void* d_out, void* d_gate, int64_t n8,
                             cudaStream_t stream);
 // attention of one new token over a paged cache, and the join of what thread blocks had of one pair (decode_kernel.cu)
-int32_t decode_rows_per_chunk(int32_t group);
+struct DecodeForm {
+    int32_t chunk_rows, tile_keys, per_sm;      // query heads of a thread block, keys of a tile, thread blocks per SM
+};
+DecodeForm decode_form(int32_t d_qk, int32_t group);
 cudaError_t launch_decode(const CUtensorMap& mk, const CUtensorMap& mv, const DecodeParams& p, int32_t d_qk, uint64_t call_tag,
                           int grid, cudaStream_t stream);
 cudaError_t launch_decode_join(const DecodeParams& p, int decode_grid, cudaStream_t stream);
