@@ -2921,23 +2921,37 @@ int32_t append_impl(const void* k, int64_t k_stride, int64_t row_elems, const vo
     return HYDRA_OK;
 }
 
-// rows of d bf16 as a 2-D map; a box is 64 columns of `rows` rows, written as 128-byte rows with the 128-byte swizzle
-int32_t make_rows_map(CUtensorMap* map, const void* base, int64_t n_rows, int32_t d, int32_t rows)
+// The pages of K or V as (64, d / 64, page_size, n_kv_heads, n_pages); a box is `rows` keys of `heads` heads of a page, written
+// head by head and key by key with the 128-byte swizzle.
+int32_t make_pages_map(CUtensorMap* map, const void* base, const hydra_paged_cache_t& c, int32_t d, int32_t rows, int32_t heads)
 {
     EncodeFn enc = encode_fn();
     if (!enc) return HYDRA_ERR_CUDA;
-    const cuuint64_t dims[2] = {static_cast<cuuint64_t>(d), static_cast<cuuint64_t>(n_rows)};
-    const cuuint64_t strides[1] = {static_cast<cuuint64_t>(d) * 2};
-    const cuuint32_t box[2] = {64, static_cast<cuuint32_t>(rows)};
-    const cuuint32_t es[2] = {1, 1};
-    const CUresult r = enc(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, const_cast<void*>(base), dims, strides, box, es,
+    const cuuint64_t row = static_cast<cuuint64_t>(d) * 2, head = row * c.page_size;
+    const cuuint64_t dims[5] = {64, static_cast<cuuint64_t>(d / 64), static_cast<cuuint64_t>(c.page_size),
+                                static_cast<cuuint64_t>(c.n_kv_heads), static_cast<cuuint64_t>(c.n_pages)};
+    const cuuint64_t strides[4] = {128, row, head, head * c.n_kv_heads};
+    const cuuint32_t box[5] = {64, static_cast<cuuint32_t>(d / 64), static_cast<cuuint32_t>(rows), static_cast<cuuint32_t>(heads), 1};
+    const cuuint32_t es[5] = {1, 1, 1, 1, 1};
+    const CUresult r = enc(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 5, const_cast<void*>(base), dims, strides, box, es,
                            CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
                            CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
     return r == CUDA_SUCCESS ? HYDRA_OK : HYDRA_ERR_CUDA;
 }
 
-// partial results: two slots per thread block, up to 32 query heads (8 or 16 if a group has no more)
-size_t decode_slot_rows(int32_t group) { return size_t{2} * DECODE_MAX_BLOCKS * (group <= 8 ? 8 : group <= 16 ? 16 : 32); }
+// K / V heads of a unit of work: as many as divide their number, up to four and up to 16 query heads
+int32_t decode_unit_kv_heads(int32_t group, int32_t n_kv_heads)
+{
+    int32_t n = 4;
+    while (n > 1 && (n_kv_heads % n || n * group > 16)) n /= 2;
+    return n;
+}
+int32_t decode_unit_rows(int32_t group, int32_t n_kv_heads) { return std::min(32, group * decode_unit_kv_heads(group, n_kv_heads)); }
+// rows of partial results: two slots per piece of the work
+size_t decode_slot_rows(int32_t group, int32_t n_kv_heads)
+{
+    return size_t{2} * DECODE_LEVELS * DECODE_MAX_BLOCKS * decode_unit_rows(group, n_kv_heads);
+}
 }  // namespace
 
 int32_t hydra_rope_axes(const void* x, int64_t x_stride, const int32_t* positions, int64_t n_tokens, int32_t n_heads,
@@ -2987,8 +3001,7 @@ int32_t hydra_mla_kv_append(const void* kv_up, int64_t kv_up_stride, const void*
 size_t hydra_workspace_bytes_decode(int32_t n_heads, int32_t n_kv_heads)
 {
     if (n_heads < 1 || n_kv_heads < 1 || n_heads % n_kv_heads) return 0;
-    const int32_t group = n_heads / n_kv_heads;
-    return kStatusBytes + decode_slot_rows(group) * (D_V + 1) * sizeof(float);
+    return kStatusBytes + sizeof(int32_t) * DECODE_LEVELS * DECODE_MAX_BLOCKS + decode_slot_rows(n_heads / n_kv_heads, n_kv_heads) * (D_V + 1) * sizeof(float);
 }
 
 int32_t hydra_attn_decode(const void* q, int64_t q_stride, const hydra_paged_cache_t* cache, int32_t n_heads, float softmax_scale,
@@ -2999,10 +3012,22 @@ int32_t hydra_attn_decode(const void* q, int64_t q_stride, const hydra_paged_cac
     if (n_heads < 1 || n_heads % c.n_kv_heads || !(softmax_scale > 0.f) || !std::isfinite(softmax_scale) ||
         q_stride < int64_t{n_heads} * c.d_qk)
         return HYDRA_ERR_INVALID_ARG;
-    const int64_t rows = int64_t{c.n_pages} * c.n_kv_heads;
-    if (!kernel_set(c.d_qk, c.d_v) || c.page_size % 8 || rows > INT32_MAX / c.page_size || q_stride % 8 ||
-        int64_t{c.n_seqs} * n_heads > INT32_MAX)
+    if (!kernel_set(c.d_qk, c.d_v) || c.page_size % 8 || q_stride % 8 || int64_t{c.n_seqs} * n_heads > INT32_MAX ||
+        int64_t{c.max_pages} * c.page_size > 1 << 30)
         return HYDRA_ERR_UNSUPPORTED;
+    DecodeParams p{};
+    p.h = n_heads;
+    p.group = n_heads / c.n_kv_heads;
+    p.unit_kv_heads = decode_unit_kv_heads(p.group, c.n_kv_heads);
+    p.unit_rows = decode_unit_rows(p.group, c.n_kv_heads);
+    p.chunks = (p.group + 31) / 32;
+    p.units = c.n_kv_heads / p.unit_kv_heads * p.chunks;
+    p.key_slices_log2 = p.unit_kv_heads == 4 ? 0 : p.unit_kv_heads == 2 ? 1 : 2;
+    p.tile_shift = 4 + p.key_slices_log2;
+    p.tile_keys = 1 << p.tile_shift;
+    p.max_len = c.max_pages * c.page_size;
+    // tiles are counted with 32 bits
+    if ((int64_t{p.max_len} / p.tile_keys + 1) * c.n_seqs > INT32_MAX / 2 / p.units) return HYDRA_ERR_UNSUPPORTED;
     if (!workspace || !aligned16(workspace)) return HYDRA_ERR_INVALID_ARG;
     if (workspace_bytes < hydra_workspace_bytes_decode(n_heads, c.n_kv_heads)) return HYDRA_ERR_WORKSPACE_TOO_SMALL;
     if (c.n_seqs > 0) {
@@ -3013,50 +3038,50 @@ int32_t hydra_attn_decode(const void* q, int64_t q_stride, const hydra_paged_cac
     if (int32_t s = device_info(&sms)) return s;
     if (c.n_seqs == 0) return HYDRA_OK;
     cudaStream_t stream = static_cast<cudaStream_t>(cuda_stream);
-    // the status block, as in the forward: marked with the call's number, or cleared where the launches are recorded
-    cudaStreamCaptureStatus capturing = cudaStreamCaptureStatusNone;
-    if (cudaStreamIsCapturing(stream, &capturing) != cudaSuccess) return HYDRA_ERR_CUDA;
-    uint64_t call_tag = 0;
-    if (capturing == cudaStreamCaptureStatusNone) call_tag = next_call_tag();
-    else if (launch_reset(static_cast<StatusBlock*>(workspace), false, stream) != cudaSuccess) return HYDRA_ERR_CUDA;
-    DecodeParams p{};
     p.q = static_cast<const uint16_t*>(q);
     p.q_stride = q_stride;
     p.page_table = c.page_table;
     p.seq_lens = c.seq_lens;
     p.out = static_cast<uint16_t*>(out);
     p.lse = lse;
-    p.h = n_heads;
-    p.kv_heads = c.n_kv_heads;
-    p.group = n_heads / c.n_kv_heads;
-    const DecodeForm form = decode_form(c.d_qk, p.group);
-    p.chunk_rows = form.chunk_rows;
-    p.chunks = (p.group + form.chunk_rows - 1) / form.chunk_rows;
-    p.tile_keys = form.tile_keys;
     uint8_t* const ws = static_cast<uint8_t*>(workspace);
-    p.part_o = reinterpret_cast<float*>(ws + kStatusBytes);
-    p.part_lse2 = p.part_o + decode_slot_rows(p.group) * D_V;
+    p.arrived = reinterpret_cast<int32_t*>(ws + kStatusBytes);
+    p.part_o = reinterpret_cast<float*>(p.arrived + DECODE_LEVELS * DECODE_MAX_BLOCKS);
+    p.part_lse2 = p.part_o + decode_slot_rows(p.group, c.n_kv_heads) * D_V;
     p.n_seqs = c.n_seqs;
     p.max_pages = c.max_pages;
     p.page_size = c.page_size;
     p.n_pages = c.n_pages;
-    p.max_len = static_cast<int32_t>(std::min<int64_t>(int64_t{c.max_pages} * c.page_size, INT32_MAX - 64));
-    p.box_rows = c.page_size % 16 ? 8 : 16;
+    p.box_rows = p.tile_keys;
+    while (c.page_size % p.box_rows) p.box_rows /= 2;
+    p.boxes = p.tile_keys / p.box_rows;
+    p.by_page = DivKeys::by(c.page_size);
+    p.blocks = std::min(sms, DECODE_MAX_BLOCKS);
+    p.by_blocks = DivKeys::by(p.blocks);
+    p.by_units = DivKeys::by(p.units);
     p.scale_log2 = softmax_scale * 1.4426950408889634f;
     p.status = static_cast<StatusBlock*>(workspace);
     p.wait_limit_ns = g_wait_limit_ns.load();
     p.debug_stall_ns = g_debug_stall_ns[HYDRA_STALL_DECODE].load();
-    CUtensorMap mk, mv;
-    if (make_rows_map(&mk, c.k, rows * c.page_size, c.d_qk, p.box_rows) || make_rows_map(&mv, c.v, rows * c.page_size, c.d_v, p.box_rows))
-        return HYDRA_ERR_CUDA;
-    const int grid = std::min(sms * form.per_sm, DECODE_MAX_BLOCKS);
+    // the status block, as in the forward: marked with the call's number, or cleared where the launches are recorded
+    cudaStreamCaptureStatus capturing = cudaStreamCaptureStatusNone;
+    if (cudaStreamIsCapturing(stream, &capturing) != cudaSuccess) return HYDRA_ERR_CUDA;
+    uint64_t call_tag = 0;
+    if (capturing == cudaStreamCaptureStatusNone) call_tag = next_call_tag();
+    else if (launch_reset(static_cast<StatusBlock*>(workspace), false, stream) != cudaSuccess) return HYDRA_ERR_CUDA;
+    CUtensorMap maps[4];
+    for (int i = 0; i < 2; ++i) {                       // whole boxes, and eight keys of a head: what a sequence has beyond them
+        const int32_t rows = i ? 8 : p.box_rows, heads = i ? 1 : p.unit_kv_heads;
+        if (make_pages_map(&maps[2 * i], c.k, c, c.d_qk, rows, heads) || make_pages_map(&maps[2 * i + 1], c.v, c, c.d_v, rows, heads))
+            return HYDRA_ERR_CUDA;
+    }
     {
         ScopedKernelTimer timer(K_FWD, stream);
-        if (launch_decode(mk, mv, p, c.d_qk, call_tag, grid, stream) != cudaSuccess) return HYDRA_ERR_CUDA;
+        if (launch_decode(maps, p, c.d_qk, call_tag, stream) != cudaSuccess) return HYDRA_ERR_CUDA;
         g_launches += 1;
     }
     ScopedKernelTimer timer(K_MERGE, stream);
-    if (launch_decode_join(p, grid, stream) != cudaSuccess) return HYDRA_ERR_CUDA;
+    if (launch_decode_join(p, stream) != cudaSuccess) return HYDRA_ERR_CUDA;
     g_launches += 1;
     return HYDRA_OK;
 }

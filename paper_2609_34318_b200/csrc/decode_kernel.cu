@@ -6,16 +6,20 @@
 // rows together. Every K / V row is needed once, 2 (d_qk + d_v) bytes for 2 g (d_qk + d_v) FLOP: memory bounds it for every
 // grouping, and what counts is that all SMs load all the time, whatever the lengths are.
 //
-// Work. The keys of a (sequence, K / V head) pair are cut into tiles of 64; all tiles of a call, one pair after the other,
-// are dealt out to the thread blocks (one per SM) in equal runs. A run covers the end of one pair, some whole pairs and the
-// beginning of another. Whole pairs are written straight to out / lse; the two cut ones leave (O, LSE) in fp32 in the
-// workspace, and hydra_decode_join_kernel joins what belongs together, in the order of the keys: results do not depend on
-// timing. The lengths are read on the device, so a captured call follows them.
+// Work. A unit is a sequence and up to four neighbouring K / V heads (their rows of a page lie side by side: a unit's loads are four
+// times as long, and its pages are looked up and translated once for all of them). Its keys are cut into tiles of 64 rows (keys
+// times heads); all tiles of a call, one unit after the other, are cut into pieces (struct Pieces): every thread block, one per
+// SM, has one of seven eighths of its share, and the rest is popped from a counter in ever smaller pieces, because SMs do not
+// read equally fast (equal shares ended up to 15 % apart). A piece covers the end of one unit, some whole units and the
+// beginning of another. Whole units are written straight to out / lse; cut ones leave (O, LSE) in fp32 in the workspace, and
+// hydra_decode_join_kernel joins what belongs together, in the order of the keys: who ran a piece changes nothing. The lengths are read on the device, so a captured call follows them.
 //
-// A thread block: one warp reads the page table and loads K, V (boxes of 16 or 8 rows, 128-byte swizzle) and, with the first
-// tile of a pair, its q rows into a ring of stages; four warps take 16 keys of every tile each, with a running maximum, sum
-// and accumulator of their own, joined once per pair. Products on mma.sync: 16 query rows (the group, padded) against 16
-// keys are far below what a tcgen05 product computes at once, and the tensor cores idle either way (1 to 16 FLOP per byte).
+// A thread block. One warp plans ahead: lengths, page table, the q rows of every unit. One thread loads the tiles into a ring. Eight
+// warps, two sets of four, take 16 rows of a tile each, one head's, with a running maximum, sum and O of their own (the sets take
+// tiles in turn, or, with more than eight query heads per K / V head, each half of the query heads). When a unit is through they
+// leave them in shared memory and each joins some of the query heads, while the ring goes on being filled.
+// Products on mma.sync: eight query heads against 16 keys are far below what a tcgen05 product computes at once, and the
+// tensor cores idle either way (1 to 16 FLOP per byte).
 #include <cuda_bf16.h>
 
 #include <algorithm>
@@ -26,35 +30,60 @@
 namespace hydra {
 namespace {
 
-constexpr int kSmemOfSm = 228 * 1024;        // of which the system takes 1 KB per thread block
+constexpr int kSlices = 4, kSlice = 16;     // a tile: four slices of 16 rows, each 16 keys of one K / V head
+constexpr int kTileRows = kSlices * kSlice;
+constexpr int kSmemLimit = 227 * 1024;
 constexpr float kRaise = 8.f;               // the running maximum is raised when it grew by more than 2^8
 
-enum : int32_t { FLAG_FIRST = 1, FLAG_LAST = 2, FLAG_END = 4, FLAG_PARTIAL = 8, FLAG_SECOND_SLOT = 16 };
-struct __align__(16) StageDesc {
+constexpr int kJoinWarps = 4, kJoinParts = 8;      // of hydra_decode_join_kernel: warps of a block, parts that a warp asks for at once
+constexpr int kJoinChunk = kJoinWarps * kJoinParts;     // parts that a block joins of a row
+
+struct __align__(16) TileDesc {
     uint64_t seen;                          // keys of the tile that count
-    int32_t item;                           // (sequence * kv_heads + kv head) * chunks + chunk
-    int32_t flags;
+    uint32_t unit;                          // number of its unit, counted over the block's pieces; or kEnd
+    uint32_t set;                           // of the warps that take it in turn
+};
+constexpr uint32_t kLastOfUnit = 1u << 31;  // added to the unit: the last of its tiles in this piece
+constexpr uint32_t kEnd = 0x7fffffffu;      // no tile is left
+struct __align__(16) UnitDesc {
+    int32_t seq, unit;                      // unit of the sequence
+    int32_t slot;                           // of a partial result; negative: the whole unit is here
+};
+// What the planning warp hands to the loading thread at a time: up to eight tiles of one unit. (No more of them: the pieces that a
+// block pops are to depend on how far it is.)
+constexpr int kBatches = 2, kBatchTiles = 8;
+struct __align__(16) BatchDesc {
+    int32_t tiles;                          // of the batch; negative: no tile is left
+    uint32_t unit;
+    int32_t left;                           // tiles of the unit in this piece, those of the batch and behind it
+    int32_t head;                           // its first K / V head
+    uint32_t set;                           // of the warps that take the first tile (by its number in the piece: which warp takes a
+};                                          // tile, and with it the order of the sums, does not depend on what the block ran before)
+struct __align__(16) BoxDesc {
+    int32_t page, row;                      // page < 0: nothing to load
+    int32_t rows;                           // that count; fewer than a box's at the end of a sequence
+    uint32_t loaded;                        // rows per head that are loaded of the box's tile
 };
 
-// Thread blocks of one kind. kNTiles: tiles of eight query heads per warp; kHeadWarps: warps that share a key's query heads;
-// kKeyWarps: warps that share a tile's keys, 16 each; kPerSm: thread blocks per SM.
-template <int kDqk_, int kNTiles_, int kHeadWarps_, int kKeyWarps_, int kPerSm_>
+// kNTiles: tiles of eight query heads per warp; kHeadSets: sets of warps that share a tile, each with query heads of its own (one:
+// the two sets take tiles in turn)
+template <int kDqk_, int kNTiles_, int kHeadSets_>
 struct Shape {
-    static constexpr int kDqk = kDqk_, kNTiles = kNTiles_, kHeadWarps = kHeadWarps_, kKeyWarps = kKeyWarps_, kPerSm = kPerSm_;
-    static constexpr int kKeys = 16 * kKeyWarps;                        // of a tile
-    static constexpr int kRows = 8 * kNTiles * kHeadWarps;              // query heads of a block
-    static constexpr int kConsumers = kKeyWarps * kHeadWarps;           // warps
-    static constexpr int kThreads = 32 * (kConsumers + 1);
-    static constexpr int kKBytes = kKeys * kDqk * 2, kVBytes = kKeys * D_V * 2, kQBytes = kRows * kDqk * 2;
-    static constexpr int kStage = kKBytes + kVBytes + kQBytes;
+    static constexpr int kDqk = kDqk_, kNTiles = kNTiles_, kHeadSets = kHeadSets_, kTurns = 2 / kHeadSets;
+    static constexpr int kWarpRows = 8 * kNTiles;                       // query heads of a warp
+    static constexpr int kRows = kNTiles * kHeadSets == 4 ? 32 : 16;    // most query heads of a unit (decode_unit_kv_heads)
+    static constexpr int kConsumers = 2 * kSlices;                      // warps
+    static constexpr int kThreads = 32 * (kConsumers + 2);
+    static constexpr int kKBytes = kTileRows * kDqk * 2, kVBytes = kTileRows * D_V * 2, kStage = kKBytes + kVBytes;
+    static constexpr int kQBytes = (kRows + kWarpRows) * kDqk * 2;      // (the last rows that a product takes may be padding)
     // floats between rows of the join buffer: 2 * 132 = 8 (mod 32), the eight values and four heads of a warp's store meet 32 banks
     static constexpr int kJoinStride = D_V + 4;
-    static constexpr int kJoin = kKeyWarps * kRows * kJoinStride * 4;
-    static constexpr int kFixed = 1024 + 512 + 16 * kKeyWarps * kRows;      // alignment of the ring; barriers and descriptors; (m, l)
-    static constexpr int kFit = (kSmemOfSm / kPerSm - 1024 - kJoin - kFixed) / kStage;
-    static constexpr int kStages = kFit < 8 ? kFit : 8;
-    static constexpr int kSmem = kStages * kStage + kJoin + 1024;
-    static_assert(kStage % 1024 == 0 && kStages >= 2, "ring");
+    static constexpr int kJoinBytes = kConsumers * kWarpRows * kJoinStride * 4;
+    static constexpr int kQSlots = kRows == 16 ? 3 : 2;                 // units that are loaded or being computed
+    static constexpr int kFixed = 1024 + 2304 + 8 * kConsumers * kWarpRows;    // alignment of the ring; barriers, descriptors; (m, l)
+    static constexpr int kStages = (kSmemLimit - kFixed - kQSlots * kQBytes - kJoinBytes) / kStage;
+    static constexpr int kSmem = kStages * kStage + kQSlots * kQBytes + kJoinBytes + 1024;
+    static_assert(kStages >= 3 && kStage % 1024 == 0 && kQBytes % 16 == 0, "ring");
 };
 
 __device__ __forceinline__ void ldmatrix_x4(uint32_t addr, uint32_t (&r)[4])
@@ -82,196 +111,388 @@ __device__ __forceinline__ void mma_bf16(float (&c)[4], const uint32_t (&a)[4], 
                  : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
                  : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
 }
+// 16 bytes of a 128-byte unit of a tile, where the 128-byte swizzle puts them (base: a multiple of 1024)
+__device__ __forceinline__ uint32_t swizzled(uint32_t base, uint32_t unit, uint32_t part)
+{
+    return base + unit * 128 + ((part ^ (unit & 7)) << 4);
+}
 __device__ __forceinline__ float neg_inf() { return __uint_as_float(0xff800000u); }
 
-// Tiles of a sequence. Lengths outside the table's reach count as its ends.
+__device__ __forceinline__ void prefetch_l2(const void* p) { asm volatile("prefetch.global.L2 [%0];" ::"l"(p)); }
+
+// Lengths outside the table's reach count as its ends.
 __device__ __forceinline__ int32_t seq_len_of(const DecodeParams& p, int32_t b)
 {
     return min(max(__ldcg(p.seq_lens + b), 0), p.max_len);
 }
-__device__ __forceinline__ int32_t tiles_of(const DecodeParams& p, int32_t len) { return (len + p.tile_keys - 1) / p.tile_keys; }
+__device__ __forceinline__ int32_t tiles_of(const DecodeParams& p, int32_t len) { return (len + p.tile_keys - 1) >> p.tile_shift; }
 
-// The run of thread block c of n: tiles [total c / n, total (c + 1) / n); the block that has tile t.
-__device__ __forceinline__ int64_t run_start(int64_t total, int64_t c, int64_t n) { return total * c / n; }
-__device__ __forceinline__ int64_t block_of(int64_t total, int64_t t, int64_t n) { return ((t + 1) * n - 1) / total; }
+// The lengths of all sequences, as a warp has read them: a lane has the sum of its share of the sequences, and the sum up to there,
+// in tiles of one unit.
+struct Lengths {
+    int32_t share, my_len, mine, sum, total;
+    static __device__ __forceinline__ int32_t scan(int32_t x, int lane)
+    {
+#pragma unroll
+        for (int d = 1; d < 32; d *= 2) {
+            const int32_t up = __shfl_up_sync(0xffffffffu, x, d);
+            if (lane >= d) x += up;
+        }
+        return x;
+    }
+    __device__ __forceinline__ Lengths(const DecodeParams& p, int lane) : share((p.n_seqs + 31) / 32), my_len(0), mine(0)
+    {
+#pragma unroll 4
+        for (int i = 0; i < share; ++i)
+            if (lane * share + i < p.n_seqs) mine += tiles_of(p, my_len = seq_len_of(p, lane * share + i));
+        sum = scan(mine, lane);
+        total = __shfl_sync(0xffffffffu, sum, 31);
+    }
+    // the sequence that has tile `at` (of one unit each), its length, and the tiles before it
+    __device__ __forceinline__ void find(const DecodeParams& p, int lane, int32_t at, int32_t& b, int32_t& len, int32_t& before) const
+    {
+        const int owner = __ffs(__ballot_sync(0xffffffffu, sum > at)) - 1;
+        before = __shfl_sync(0xffffffffu, sum - mine, owner);
+        if (share == 1) {
+            b = owner;
+            len = __shfl_sync(0xffffffffu, my_len, owner);
+            return;
+        }
+        for (b = owner * share;; b += 32) {
+            const int32_t its = b + lane < p.n_seqs ? seq_len_of(p, b + lane) : 0, n = tiles_of(p, its), s = scan(n, lane);
+            const uint32_t past = __ballot_sync(0xffffffffu, before + s > at);
+            if (past) {
+                const int first = __ffs(past) - 1;
+                b += first;
+                len = __shfl_sync(0xffffffffu, its, first);
+                before += __shfl_sync(0xffffffffu, s - n, first);
+                return;
+            }
+            before += __shfl_sync(0xffffffffu, s, 31);
+        }
+    }
+};
 
-struct Start { int32_t seq; int32_t pad; int64_t before; int64_t total; };
+// How the tiles of a call are cut: into equal shares, one per thread block, and a share of 32 tiles or more into pieces of 7/8,
+// 1/16, 1/32, 1/64 and 1/64 of it, which are run in that order: the first pieces of all shares, then the second ones, ... Pieces are
+// numbered in the order of their tiles.
+struct Pieces {
+    int32_t total, blocks, share, levels, start[DECODE_LEVELS + 1];
+    __device__ __forceinline__ Pieces(const DecodeParams& p, int32_t tiles_of_a_unit)
+        : total(tiles_of_a_unit * p.units), blocks(p.blocks), share(p.by_blocks(total + p.blocks - 1))
+    {
+        levels = share < 32 ? 1 : DECODE_LEVELS;
+        start[0] = 0;
+#pragma unroll
+        for (int l = 1; l <= DECODE_LEVELS; ++l) start[l] = share - (l < levels ? share >> (l + 2) : 0);
+    }
+    __device__ __forceinline__ int32_t count() const { return total ? (total + share - 1) / share * levels : 0; }
+    // the i-th piece to be run: its number and tiles (none: it lies behind the end)
+    __device__ __forceinline__ int32_t in_order(int32_t i, int32_t& lo, int32_t& hi) const
+    {
+        int32_t level = 0, of = i;
+        for (; of >= blocks; of -= blocks) ++level;
+        range(of, level, lo, hi);
+        return of * levels + level;
+    }
+    __device__ __forceinline__ void range(int32_t piece, int32_t& lo, int32_t& hi) const
+    {
+        const int32_t of = piece / levels;
+        range(of, piece - of * levels, lo, hi);
+    }
+    __device__ __forceinline__ void range(int32_t of, int32_t level, int32_t& lo, int32_t& hi) const
+    {
+        lo = hi = 0;
+#pragma unroll
+        for (int l = 0; l < DECODE_LEVELS; ++l)
+            if (l == level) { lo = start[l]; hi = start[l + 1]; }
+        lo = min(of * share + lo, total);
+        hi = min(of * share + hi, total);
+    }
+    __device__ __forceinline__ int32_t piece_of(int32_t tile) const
+    {
+        const int32_t of = tile / share, at = tile - of * share;
+        int32_t level = 0;
+#pragma unroll
+        for (int l = 1; l < DECODE_LEVELS; ++l) level += l < levels && at >= start[l] ? 1 : 0;
+        return of * levels + level;
+    }
+};
+
+// The counter of popped pieces: the call's number above kCountBits, the count below. Whatever a workspace held before counts as
+// zero; where the launches are recorded the number is zero and a launch of their own clears it. `old` is what atomicAdd(word, 1)
+// has returned; the result is the count before it.
+constexpr int kCountBits = 20;
+__device__ __forceinline__ int32_t popped(unsigned long long* word, unsigned long long old, uint64_t call_tag)
+{
+    const unsigned long long tag = call_tag >> kCountBits;
+    while (old >> kCountBits != tag) {
+        const unsigned long long seen = atomicCAS(word, old + 1, (tag << kCountBits) + 1);
+        if (seen == old + 1) return 0;
+        old = seen >> kCountBits == tag ? atomicAdd(word, 1ull) : seen - 1;
+    }
+    return static_cast<int32_t>(old & ((1u << kCountBits) - 1));
+}
+
+// What (O, log2 of the sum) of several parts is together; 0 and -inf of none
+struct Joined { float4 o; float lse2; };
+template <int kN>
+__device__ __forceinline__ Joined join_of(const float (&part)[kN], const float4 (&x)[kN])
+{
+    float top = part[0];
+#pragma unroll
+    for (int j = 1; j < kN; ++j) top = fmaxf(top, part[j]);
+    const float ref = top == neg_inf() ? 0.f : top;
+    float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
+    float sum = 0.f;
+#pragma unroll
+    for (int j = 0; j < kN; ++j) {
+        const float f = ex2_approx(part[j] - ref);
+        sum += f;
+        o.x += f * x[j].x; o.y += f * x[j].y; o.z += f * x[j].z; o.w += f * x[j].w;
+    }
+    const float inv = top == neg_inf() ? 0.f : 1.f / sum;
+    return {make_float4(o.x * inv, o.y * inv, o.z * inv, o.w * inv), top == neg_inf() ? top : top + log2f(sum)};
+}
 
 template <class S>
-__global__ void __launch_bounds__(S::kThreads, S::kPerSm)
-hydra_decode_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_v, const DecodeParams p,
+__global__ void __launch_bounds__(S::kThreads, 1)
+hydra_decode_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_v,
+                    const __grid_constant__ CUtensorMap map_k8, const __grid_constant__ CUtensorMap map_v8, const DecodeParams p,
                     const uint64_t call_tag)
 {
-    constexpr int kDqk = S::kDqk, kKeys = S::kKeys, kKeyWarps = S::kKeyWarps, kNT = S::kNTiles;
-    constexpr int kBoxesK = kDqk / 64, kBoxesV = D_V / 64, kBox = kKeys * 128;      // 64 columns of a tile
+    constexpr int kDqk = S::kDqk, kNT = S::kNTiles;
+    constexpr uint32_t kUnitsK = kDqk / 64, kUnitsV = D_V / 64;      // 128-byte units of a row
     extern __shared__ uint8_t smem_raw[];
-    __shared__ __align__(8) uint64_t bars[2 * S::kStages + 2];
-    __shared__ StageDesc s_desc[S::kStages];
-    __shared__ float2 s_ml[2][kKeyWarps][S::kRows];      // of two pairs in turn: the slowest warp may still read the last one's
-    __shared__ int64_t s_scan[S::kThreads / 32];
-    __shared__ Start s_start;
+    enum { B_FULL = 0, B_EMPTY = S::kStages, B_QFULL = 2 * S::kStages, B_QEMPTY = B_QFULL + S::kQSlots, B_JFULL = B_QEMPTY + S::kQSlots,
+           B_JEMPTY, B_BFULL, B_BEMPTY = B_BFULL + kBatches,
+           B_COUNT = B_BEMPTY + kBatches };
+    __shared__ __align__(8) uint64_t bars[B_COUNT];
+    __shared__ TileDesc s_tile[S::kStages];
+    __shared__ UnitDesc s_unit[S::kQSlots];
+    __shared__ BatchDesc s_batch[kBatches];
+    __shared__ BoxDesc s_box[kBatches][32];
+    __shared__ float2 s_ml[S::kConsumers][S::kWarpRows];
     __shared__ int abort_flag;
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
-    const uint32_t ring = (smem_u32(smem_raw) + 1023u) & ~1023u;
-    float* const join = reinterpret_cast<float*>(smem_raw + (ring - smem_u32(smem_raw)) + S::kStages * S::kStage);
-    auto full = [&](int s) { return smem_u32(&bars[s]); };
-    auto empty = [&](int s) { return smem_u32(&bars[S::kStages + s]); };
-    const uint32_t join_bar[2] = {smem_u32(&bars[2 * S::kStages]), smem_u32(&bars[2 * S::kStages + 1])};
+    const uint32_t ring = (smem_u32(smem_raw) + 1023u) & ~1023u, q_ring = ring + S::kStages * S::kStage;
+    float* const join = reinterpret_cast<float*>(smem_raw + (q_ring - smem_u32(smem_raw)) + S::kQSlots * S::kQBytes);
+    auto bar = [&](int i) { return smem_u32(&bars[i]); };
     if (tid == 0) {
-        for (int s = 0; s < S::kStages; ++s) { mbar_init(full(s), 1); mbar_init(empty(s), S::kConsumers); }
-        mbar_init(join_bar[0], S::kConsumers);
-        mbar_init(join_bar[1], S::kConsumers);
+        for (int i = 0; i < S::kStages; ++i) { mbar_init(bar(B_FULL + i), 1); mbar_init(bar(B_EMPTY + i), S::kConsumers); }
+        for (int i = 0; i < S::kQSlots; ++i) { mbar_init(bar(B_QFULL + i), 1); mbar_init(bar(B_QEMPTY + i), S::kConsumers); }
+        mbar_init(bar(B_JFULL), S::kConsumers);
+        mbar_init(bar(B_JEMPTY), S::kConsumers);
+        for (int i = 0; i < kBatches; ++i) { mbar_init(bar(B_BFULL + i), 1); mbar_init(bar(B_BEMPTY + i), 1); }
         fence_mbar_init();
-        tma_prefetch_desc(&map_k);
-        tma_prefetch_desc(&map_v);
+        tma_prefetch_desc(&map_k); tma_prefetch_desc(&map_v); tma_prefetch_desc(&map_k8); tma_prefetch_desc(&map_v8);
         abort_flag = 0;
-        s_start.total = 0;
     }
+    __syncthreads();
     wait_for_previous_launch();
     overlap_next_launch();                              // (the join's blocks wait for this grid's end)
     if (call_tag && blockIdx.x == 0 && tid == 0) {      // nothing has cleared the status block
         p.status->call_tag = call_tag;
         for (int i = 0; i < 4; ++i) p.status->probe_cycles[i] = p.status->probe_ns[i] = 0;
     }
-
-    // ------------------------------------------------------------------ this block's run of tiles
-    const int32_t per_seq = p.kv_heads * p.chunks;      // pairs of a sequence
-    int64_t n_blocks;
-    {
-        const int per = (p.n_seqs + S::kThreads - 1) / S::kThreads;
-        const int b0 = min(tid * per, p.n_seqs), b1 = min(b0 + per, p.n_seqs);
-        int64_t mine = 0;
-        for (int b = b0; b < b1; ++b) mine += tiles_of(p, seq_len_of(p, b));
-        int64_t sum = mine;
-#pragma unroll
-        for (int d = 1; d < 32; d *= 2) {
-            const int64_t up = __shfl_up_sync(0xffffffffu, sum, d);
-            if (lane >= d) sum += up;
-        }
-        if (lane == 31) s_scan[warp] = sum;
-        __syncthreads();
-        int64_t before = sum - mine, all = 0;
-        for (int w = 0; w < S::kThreads / 32; ++w) {
-            if (w < warp) before += s_scan[w];
-            all += s_scan[w];
-        }
-        const int64_t total = all * per_seq;
-        n_blocks = min(static_cast<int64_t>(gridDim.x), total);
-        if (blockIdx.x >= n_blocks) return;
-        const int64_t first = run_start(total, blockIdx.x, n_blocks) / per_seq;     // in tiles of a head
-        if (first >= before && first < before + mine) {
-            int64_t at = before;
-            int b = b0;
-            for (;; ++b) {
-                const int n = tiles_of(p, seq_len_of(p, b));
-                if (first < at + n) break;
-                at += n;
-            }
-            s_start.seq = b;
-            s_start.before = at;
-            s_start.total = total;
-        }
-        __syncthreads();
-    }
-    const int64_t total = s_start.total;
-    const int64_t lo = run_start(total, blockIdx.x, n_blocks), hi = run_start(total, blockIdx.x + 1, n_blocks);
+    // The page table into L2 while the lengths are on their way (a line per thread, more is left to the lookups).
+    if (const int64_t at = (static_cast<int64_t>(tid) * gridDim.x + blockIdx.x) * 32; at < static_cast<int64_t>(p.n_seqs) * p.max_pages)
+        prefetch_l2(p.page_table + at);
     const uint64_t limit = p.wait_limit_ns;
     volatile int* abort_p = &abort_flag;
+    auto wait = [&](int i, uint32_t parity) { return mbar_wait(bar(i), parity & 1u, abort_p, limit); };
 
     if (warp == S::kConsumers) {
-        // ------------------------------------------------------------------ page table and loads
+        // ------------------------------------------------------------------ pieces, page table, q
+        // Runs ahead of the loading thread, which must not wait for anything but places in the ring: what it does not issue for a
+        // moment, the memory does not catch up on.
         if (p.debug_stall_ns) {
-            debug_stall(p.debug_stall_ns);              // test hook: load nothing; the other warps' waits run out
+            debug_stall(p.debug_stall_ns);              // test hook: plan nothing; the other warps' waits run out
         } else {
-            const int32_t boxes = kKeys / p.box_rows;   // of a tile; lane j asks for box j's page
-            const int32_t key_in_tile = lane * p.box_rows;
-            int32_t b = s_start.seq, len = seq_len_of(p, b), n_tiles = tiles_of(p, len);
-            int64_t base = s_start.before * per_seq;    // first tile of sequence b
-            int32_t in_seq = static_cast<int32_t>((lo - base) / n_tiles);           // pair of the sequence, and tile of the pair
-            int32_t tile = static_cast<int32_t>((lo - base) - static_cast<int64_t>(in_seq) * n_tiles);
-            auto page_at = [&](int32_t seq, int32_t key, int32_t seq_len) -> int32_t {
-                return lane < boxes && key < seq_len ? __ldcg(p.page_table + static_cast<int64_t>(seq) * p.max_pages + key / p.page_size) : -1;
-            };
-            int32_t page = page_at(b, tile * kKeys + key_in_tile, len);
+            const Lengths lengths(p, lane);
+            const Pieces pieces(p, lengths.total);
+            const int32_t box_rows = p.box_rows, boxes = p.boxes, most = min(kBatchTiles, 32 / boxes);
+            unsigned long long* const counter = reinterpret_cast<unsigned long long*>(&p.status->pieces);
+            uint32_t n_unit = 0, n_batch = 0;           // of this block so far
             bool ok = true;
-            for (int64_t t = lo; t <= hi; ++t) {
-                const int st = static_cast<int>((t - lo) % S::kStages);
-                const uint32_t turn = static_cast<uint32_t>((t - lo) / S::kStages);
-                if (lane == 0) ok = mbar_wait(empty(st), (turn & 1u) ^ 1u, abort_p, limit);
+            auto hand_over = [&](const BatchDesc& d, const BoxDesc& box) {
+                const uint32_t at = n_batch % kBatches;
+                if (lane == 0) ok = wait(B_BEMPTY + at, (n_batch / kBatches) ^ 1u);
                 ok = __shfl_sync(0xffffffffu, ok, 0);
-                if (!ok) break;
-                if (t == hi) {
-                    if (lane == 0) { s_desc[st].flags = FLAG_END; mbar_arrive(full(st)); }
-                    break;
-                }
-                const int32_t key = tile * kKeys + key_in_tile;
-                const bool there = lane < boxes && key < len && page >= 0 && page < p.n_pages;
-                const uint64_t mask = there ? (~0ull >> (64 - min(p.box_rows, len - key))) << key_in_tile : 0ull;
-                const uint32_t seen_lo = __reduce_or_sync(0xffffffffu, static_cast<uint32_t>(mask));
-                const uint32_t seen_hi = __reduce_or_sync(0xffffffffu, static_cast<uint32_t>(mask >> 32));
-                const int n_boxes = __popc(__ballot_sync(0xffffffffu, there));
-                const bool first = tile == 0 || t == lo, last = tile == n_tiles - 1 || t == hi - 1;
-                const int32_t kvh = in_seq / p.chunks, chunk = in_seq - kvh * p.chunks;
-                const int32_t q_rows = min(S::kRows, p.group - chunk * S::kRows);
-                const uint32_t stage = ring + static_cast<uint32_t>(st) * S::kStage;
-                if (lane == 0) {
-                    // does another block have tiles of this pair?
-                    const int64_t pair0 = t - tile;
-                    const bool cut = pair0 < lo || pair0 + n_tiles > hi;
-                    s_desc[st].seen = static_cast<uint64_t>(seen_hi) << 32 | seen_lo;
-                    s_desc[st].item = b * per_seq + in_seq;
-                    s_desc[st].flags = (first ? FLAG_FIRST : 0) | (last ? FLAG_LAST : 0) | (cut ? FLAG_PARTIAL : 0) |
-                                       (pair0 >= lo ? FLAG_SECOND_SLOT : 0);
-                    const uint32_t q_bytes = first ? static_cast<uint32_t>(q_rows) * kDqk * 2 : 0u;
-                    mbar_arrive_expect_tx(full(st), static_cast<uint32_t>(n_boxes * p.box_rows) * (kDqk + D_V) * 2 + q_bytes);
-                    if (first)
-                        bulk_load(stage + S::kKBytes + S::kVBytes,
-                                  p.q + b * p.q_stride + static_cast<int64_t>(kvh * p.group + chunk * S::kRows) * kDqk, q_bytes, full(st));
-                }
-                __syncwarp();
-                if (there) {
-                    const int32_t row = static_cast<int32_t>((static_cast<int64_t>(page) * p.kv_heads + kvh) * p.page_size + key % p.page_size);
-                    const uint32_t dst = stage + static_cast<uint32_t>(key_in_tile) * 128;
-#pragma unroll
-                    for (int c = 0; c < kBoxesK; ++c) tma_load_2d(dst + c * kBox, &map_k, full(st), c * 64, row);
-#pragma unroll
-                    for (int c = 0; c < kBoxesV; ++c) tma_load_2d(dst + S::kKBytes + c * kBox, &map_v, full(st), c * 64, row);
-                }
-                // the next tile, and its pages while the ring is waited for
-                if (++tile == n_tiles) {
-                    tile = 0;
-                    if (++in_seq == per_seq) {
-                        in_seq = 0;
-                        if (t + 1 < hi) {
+                if (!ok) return;
+                s_box[at][lane] = box;
+                if (lane == 0) s_batch[at] = d;
+                mbar_arrive_warp(bar(B_BFULL + at));
+                ++n_batch;
+            };
+            auto plan = [&](int32_t piece, int32_t lo, int32_t hi) {
+                int32_t b, before, len;
+                lengths.find(p, lane, p.by_units(lo), b, len, before);
+                int32_t n_tiles = tiles_of(p, len);
+                const int32_t in_seq = lo - before * p.units;
+                int32_t unit = in_seq / n_tiles, tile = in_seq - unit * n_tiles;        // of the sequence, of the unit
+                if (lane == 0) p.arrived[piece] = 0;    // (for the join, which counts with it)
+                for (int32_t t = lo; t < hi && ok;) {
+                    // ------------------------------------------------ a unit's tiles in this piece: q rows, what the joining warp needs
+                    int32_t left = min(n_tiles - tile, hi - t);
+                    const int32_t end = t += left;
+                    if (lane == 0) {
+                        const int32_t q_slot = n_unit % S::kQSlots, head0 = p.first_head(unit), rows = p.rows_of(unit);
+                        ok = wait(B_QEMPTY + q_slot, (n_unit / S::kQSlots) ^ 1u);
+                        if (ok) {
+                            s_unit[q_slot] = {b, unit, left < n_tiles ? 2 * piece + (tile == 0 ? 1 : 0) : -1};
+                            mbar_arrive_expect_tx(bar(B_QFULL + q_slot), static_cast<uint32_t>(rows) * kDqk * 2);
+                            bulk_load(q_ring + static_cast<uint32_t>(q_slot) * S::kQBytes,
+                                      p.q + b * p.q_stride + static_cast<int64_t>(head0) * kDqk,
+                                      static_cast<uint32_t>(rows) * kDqk * 2, bar(B_QFULL + q_slot));
+                        }
+                    }
+                    ok = __shfl_sync(0xffffffffu, ok, 0);
+                    while (left > 0 && ok) {
+                        const int32_t n = min(left, most), key = (tile << p.tile_shift) + lane * box_rows;
+                        const int32_t rows = lane < n * boxes ? min(box_rows, len - key) : 0;
+                        BoxDesc box{-1, 0, rows, 0u};
+                        if (rows > 0) {
+                            const int32_t col = p.by_page(key);
+                            const int32_t page = __ldcg(p.page_table + static_cast<int64_t>(b) * p.max_pages + col);
+                            if (page >= 0 && page < p.n_pages) {
+                                box.page = page;
+                                box.row = key - col * p.page_size;
+                                box.loaded = static_cast<uint32_t>((rows + 7) & ~7);
+                            }
+                        }
+                        for (int d = 1; d < boxes; d *= 2) box.loaded += __shfl_xor_sync(0xffffffffu, box.loaded, d);
+                        hand_over({n, n_unit, left, p.first_kv_head(unit), static_cast<uint32_t>(end - left - lo) % S::kTurns}, box);
+                        tile += n;
+                        left -= n;
+                    }
+                    ++n_unit;
+                    if (tile == n_tiles) {
+                        tile = 0;
+                        if (++unit == p.units && t < hi) {
+                            unit = 0;
                             do { len = seq_len_of(p, ++b); } while (len == 0);
                             n_tiles = tiles_of(p, len);
                         }
                     }
                 }
-                if (t + 1 < hi) page = page_at(b, tile * kKeys + key_in_tile, len);
+            };
+            for (int32_t i = blockIdx.x; ok && i < pieces.levels * pieces.blocks;) {
+                unsigned long long pop = 0;
+                const bool more = pieces.levels > 1;
+                if (more && lane == 0) pop = atomicAdd(counter, 1ull);          // (looked at when this piece has been planned)
+                int32_t lo, hi;
+                const int32_t piece = pieces.in_order(i, lo, hi);
+                i = more ? -1 : INT32_MAX;
+                if (lo < hi) plan(piece, lo, hi);
+                if (more) {
+                    if (lane == 0) i = pieces.blocks + popped(counter, pop, call_tag);
+                    i = __shfl_sync(0xffffffffu, i, 0);
+                }
+            }
+            if (ok) hand_over({-1, 0u, 0, 0, 0u}, {});          // no tile is left
+        }
+    } else if (warp == S::kConsumers + 1) {
+        // ------------------------------------------------------------------ loads
+        if (elect_one()) {
+            const int32_t box_rows = p.box_rows, boxes = p.boxes;
+            const uint32_t row_bytes = static_cast<uint32_t>(p.unit_kv_heads) * (kDqk + D_V) * 2;      // of a key
+            const uint32_t k_box = static_cast<uint32_t>(box_rows * p.unit_kv_heads) * kDqk * 2, v_box = static_cast<uint32_t>(box_rows * p.unit_kv_heads) * D_V * 2;
+            uint32_t st = 0, turn = 0;                  // place in the ring
+            bool ok = true;
+            for (uint32_t n_batch = 0; ok; ++n_batch) {
+                const uint32_t at = n_batch % kBatches;
+                ok = wait(B_BFULL + at, n_batch / kBatches);
+                if (!ok) break;
+                const BatchDesc batch = s_batch[at];
+                if (batch.tiles < 0) {
+                    if (wait(B_EMPTY + st, turn ^ 1u)) {
+                        s_tile[st].unit = kEnd;
+                        mbar_arrive(bar(B_FULL + st));
+                    }
+                    break;
+                }
+                for (int32_t i = 0; i < batch.tiles; ++i) {
+                    BoxDesc d = s_box[at][i * boxes];
+                    ok = wait(B_EMPTY + st, turn ^ 1u);
+                    if (!ok) break;
+                    const uint32_t full = bar(B_FULL + st);
+                    uint32_t k_dst = ring + st * S::kStage, v_dst = k_dst + S::kKBytes;
+                    uint64_t seen = 0;
+                    mbar_expect_tx(full, d.loaded * row_bytes);
+                    for (int32_t j = 0; j < boxes; ++j, k_dst += k_box, v_dst += v_box) {
+                        if (j) d = s_box[at][i * boxes + j];
+                        if (d.page < 0) continue;
+                        seen |= (~0ull >> (64 - d.rows)) << (j * box_rows);
+                        if (d.rows == box_rows) {
+                            tma_load_5d(k_dst, &map_k, full, 0, 0, d.row, batch.head, d.page);
+                            tma_load_5d(v_dst, &map_v, full, 0, 0, d.row, batch.head, d.page);
+                        } else {                        // the last rows of a sequence: eight at a time, head by head
+                            for (int32_t h = 0; h < p.unit_kv_heads; ++h)
+                                for (int32_t r = 0; r < d.rows; r += 8) {
+                                    const uint32_t to = static_cast<uint32_t>(h * box_rows + r);
+                                    tma_load_5d(k_dst + to * kDqk * 2, &map_k8, full, 0, 0, d.row + r, batch.head + h, d.page);
+                                    tma_load_5d(v_dst + to * D_V * 2, &map_v8, full, 0, 0, d.row + r, batch.head + h, d.page);
+                                }
+                        }
+                    }
+                    s_tile[st].seen = seen;
+                    s_tile[st].unit = batch.unit | (batch.left - i == 1 ? kLastOfUnit : 0u);
+                    s_tile[st].set = (batch.set + i) % S::kTurns;
+                    mbar_arrive(full);
+                    if (++st == S::kStages) { st = 0; ++turn; }
+                }
+                mbar_arrive(bar(B_BEMPTY + at));
             }
         }
     } else {
         // ------------------------------------------------------------------ scores, softmax, O
         // Keys stand on the 16 rows of a product and query heads on its 8 columns: S^T = K Q^T, O^T = V^T P^T. A thread has the
         // heads 2 (lane mod 4) and the one after it, of every tile of eight, and of a product the rows lane / 4 and 8 more.
-        const int kw = warp % kKeyWarps, head_of_warp = warp / kKeyWarps * 8 * kNT, key_of_lane = lane >> 2;
+        const int slice = warp % kSlices, key_of_lane = lane >> 2;
+        const uint32_t set = warp / kSlices;
+        const int first_row = S::kHeadSets == 1 ? 0 : set * S::kWarpRows;      // of its K / V head's query heads
+        const int kv_head = slice >> p.key_slices_log2, key_slice = slice & ((1 << p.key_slices_log2) - 1);     // of the unit, of its head
+        const int q_row = kv_head * p.group + first_row;
+        // Rows of the tile: boxes one after the other, in a box head by head. Of the slice's 16 keys, this lane addresses key r.
+        auto tile_row = [&](int r) {
+            const int key = key_slice * kSlice + r, box = key / p.box_rows;
+            return static_cast<uint32_t>((box * p.unit_kv_heads + kv_head) * p.box_rows + key - box * p.box_rows);
+        };
+        const uint32_t k_unit0 = tile_row(lane & 15) * kUnitsK, k_part = (lane >> 4) & 1;
+        const uint32_t v_unit0 = tile_row((lane & 7) + ((lane >> 4) & 1) * 8) * kUnitsV, v_part = (lane >> 3) & 1;
         uint32_t q[kDqk / 16][kNT][2];
         float o[D_V / 16][kNT][4];
         float m[kNT][2], l[kNT][2];
-        const uint32_t k_row = static_cast<uint32_t>(kw * 16 + (lane & 15)), k_unit = (lane >> 4) & 1;
-        const uint32_t v_row = static_cast<uint32_t>(kw * 16 + (lane & 7) + ((lane >> 4) & 1) * 8), v_unit = (lane >> 3) & 1;
-        uint32_t joins = 0;
+        if (warp == 0)                                  // sequences without a key
+            for (int32_t b0 = blockIdx.x; b0 < p.n_seqs; b0 += 32 * gridDim.x) {
+                const int32_t mine = b0 + lane * gridDim.x;
+                uint32_t none = __ballot_sync(0xffffffffu, mine < p.n_seqs && seq_len_of(p, mine) == 0);
+                for (; none; none &= none - 1) {
+                    const int32_t b = b0 + (__ffs(none) - 1) * gridDim.x;
+                    for (int32_t a = 0; a < p.h; ++a) {
+                        reinterpret_cast<uint2*>(p.out + (static_cast<int64_t>(b) * p.h + a) * D_V)[lane] = make_uint2(0u, 0u);
+                        if (lane == 0) p.lse[static_cast<int64_t>(a) * p.n_seqs + b] = neg_inf();
+                    }
+                }
+            }
+        const int key_slices = 1 << p.key_slices_log2;
+        UnitDesc of{};
+        uint32_t unit = kEnd;
         for (uint32_t n = 0;; ++n) {
             const int st = static_cast<int>(n % S::kStages);
-            if (!mbar_wait(full(st), (n / S::kStages) & 1u, abort_p, limit)) break;
-            const StageDesc d = s_desc[st];
-            if (d.flags & FLAG_END) break;
-            const uint32_t stage = ring + static_cast<uint32_t>(st) * S::kStage;
-            if (d.flags & FLAG_FIRST) {
+            if (!wait(B_FULL + st, n / S::kStages)) break;
+            const TileDesc d = s_tile[st];
+            if (d.unit == kEnd) break;
+            if ((d.unit & ~kLastOfUnit) != unit) {
+                unit = d.unit & ~kLastOfUnit;
+                const int q_slot = static_cast<int>(unit % S::kQSlots);
+                if (!wait(B_QFULL + q_slot, unit / S::kQSlots)) break;
+                of = s_unit[q_slot];
 #pragma unroll
                 for (int t = 0; t < kNT; ++t) {
-                    const uint32_t q_at = stage + S::kKBytes + S::kVBytes + static_cast<uint32_t>(head_of_warp + t * 8 + (lane & 7)) * (kDqk * 2) + (lane >> 3) * 16;
+                    const uint32_t q_at = q_ring + static_cast<uint32_t>(q_slot) * S::kQBytes +
+                                          static_cast<uint32_t>(q_row + t * 8 + (lane & 7)) * (kDqk * 2) + (lane >> 3) * 16;
 #pragma unroll
                     for (int ks = 0; ks < kDqk / 16; ks += 2) {
                         uint32_t f[4];
@@ -279,6 +500,7 @@ hydra_decode_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_cons
                         q[ks][t][0] = f[0]; q[ks][t][1] = f[1]; q[ks + 1][t][0] = f[2]; q[ks + 1][t][1] = f[3];
                     }
                 }
+                mbar_arrive_warp(bar(B_QEMPTY + q_slot));
 #pragma unroll
                 for (int i = 0; i < D_V / 16 * kNT * 4; ++i) o[i / (4 * kNT)][i / 4 % kNT][i % 4] = 0.f;
 #pragma unroll
@@ -287,15 +509,16 @@ hydra_decode_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_cons
                     l[t][0] = l[t][1] = 0.f;
                 }
             }
-            const uint32_t seen = static_cast<uint32_t>(d.seen >> (kw * 16)) & 0xffffu;
-            if (seen) {
+            const uint32_t seen = static_cast<uint32_t>(d.seen >> (key_slice * kSlice)) & 0xffffu;
+            if (seen && (S::kTurns == 1 || d.set == set)) {
+                const uint32_t stage = ring + static_cast<uint32_t>(st) * S::kStage;
                 float s[2][kNT][4];                     // even and odd steps: two chains of products per tile of heads
 #pragma unroll
                 for (int i = 0; i < 8 * kNT; ++i) s[i / (4 * kNT)][i / 4 % kNT][i % 4] = 0.f;
 #pragma unroll
                 for (int ks = 0; ks < kDqk / 16; ++ks) {
                     uint32_t kf[4];
-                    ldmatrix_x4(stage + (ks / 4) * kBox + k_row * 128 + ((((ks % 4) * 2 + k_unit) ^ (k_row & 7)) << 4), kf);
+                    ldmatrix_x4(swizzled(stage, k_unit0 + ks / 4, ks % 4 * 2 + k_part), kf);
 #pragma unroll
                     for (int t = 0; t < kNT; ++t) mma_bf16(s[ks & 1][t], kf, q[ks][t][0], q[ks][t][1]);
                 }
@@ -311,26 +534,25 @@ hydra_decode_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_cons
                     }
                     // The reference of the exponentials is raised when a score is more than 2^8 above it: until then, no warp-wide
                     // maximum is needed, one vote says so.
-                    const float top0 = fmaxf(x[0], x[2]), top1 = fmaxf(x[1], x[3]);
-                    if (__any_sync(0xffffffffu, top0 > m[t][0] + kRaise || top1 > m[t][1] + kRaise)) {
+                    float top[2] = {fmaxf(x[0], x[2]), fmaxf(x[1], x[3])};
+                    if (__any_sync(0xffffffffu, top[0] > m[t][0] + kRaise || top[1] > m[t][1] + kRaise)) {
 #pragma unroll
                         for (int c = 0; c < 2; ++c) {
-                            float top = c ? top1 : top0;
 #pragma unroll
-                            for (int g = 4; g < 32; g *= 2) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, g));
-                            if (top > m[t][c] + kRaise) {
-                                const float f = ex2_approx(m[t][c] - top);
-                                m[t][c] = top;
+                            for (int g = 4; g < 32; g *= 2) top[c] = fmaxf(top[c], __shfl_xor_sync(0xffffffffu, top[c], g));
+                            if (top[c] > m[t][c] + kRaise) {
+                                const float f = ex2_approx(m[t][c] - top[c]);
+                                m[t][c] = top[c];
                                 l[t][c] *= f;
 #pragma unroll
                                 for (int j = 0; j < D_V / 16; ++j) { o[j][t][c] *= f; o[j][t][c + 2] *= f; }
                             }
                         }
                     }
-                    const float ref0 = m[t][0] == neg_inf() ? 0.f : m[t][0], ref1 = m[t][1] == neg_inf() ? 0.f : m[t][1];
+                    const float ref[2] = {m[t][0] == neg_inf() ? 0.f : m[t][0], m[t][1] == neg_inf() ? 0.f : m[t][1]};
                     float pr[4];
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) pr[e] = ex2_approx(x[e] - (e & 1 ? ref1 : ref0));
+                    for (int e = 0; e < 4; ++e) pr[e] = ex2_approx(x[e] - ref[e & 1]);
                     l[t][0] += pr[0] + pr[2];
                     l[t][1] += pr[1] + pr[3];
                     // P as the sum of two bf16 (2^-17 of it is lost): the tensor cores have time for a second product, and with
@@ -342,14 +564,14 @@ hydra_decode_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_cons
                         pl[t][e] = transpose_8x8(pack_bf16x2(pr[2 * e] - __uint_as_float(h << 16), pr[2 * e + 1] - __uint_as_float(h & 0xffff0000u)));
                     }
                 }
-                // rows behind the end hold anything: 0 * NaN must not reach the sums
+                // rows that do not count hold anything: 0 * NaN must not reach the sums
                 const uint32_t v_bits = seen >> (2 * (lane & 3));
                 const uint32_t keep0 = (v_bits & 1u ? 0xffffu : 0u) | (v_bits & 2u ? 0xffff0000u : 0u);
                 const uint32_t keep1 = (v_bits & 0x100u ? 0xffffu : 0u) | (v_bits & 0x200u ? 0xffff0000u : 0u);
 #pragma unroll
                 for (int j = 0; j < D_V / 16; ++j) {
                     uint32_t vf[4];
-                    ldmatrix_x4_trans(stage + S::kKBytes + (j / 4) * kBox + v_row * 128 + ((((j % 4) * 2 + v_unit) ^ (v_row & 7)) << 4), vf);
+                    ldmatrix_x4_trans(swizzled(stage + S::kKBytes, v_unit0 + j / 4, j % 4 * 2 + v_part), vf);
                     if (seen != 0xffffu) { vf[0] &= keep0; vf[1] &= keep0; vf[2] &= keep1; vf[3] &= keep1; }
 #pragma unroll
                     for (int t = 0; t < kNT; ++t) {
@@ -358,67 +580,67 @@ hydra_decode_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_cons
                     }
                 }
             }
-            mbar_arrive_warp(empty(st));
-            if (!(d.flags & FLAG_LAST)) continue;
-
-            // ---------------------------------------------------------------- the warps' shares of the pair, joined
-            const int32_t chunk = d.item % p.chunks, bh = d.item / p.chunks, b = bh / p.kv_heads, kvh = bh - b * p.kv_heads;
-            const int32_t head0 = kvh * p.group + chunk * S::kRows, q_rows = min(S::kRows, p.group - chunk * S::kRows);
-            auto& ml_of = s_ml[joins & 1u];
+            mbar_arrive_warp(bar(B_EMPTY + st));
+            if (!(d.unit & kLastOfUnit)) continue;
+            // ---------------------------------------------------------------- what the warp has of its unit, into shared memory
 #pragma unroll
             for (int t = 0; t < kNT; ++t)
 #pragma unroll
-                for (int c = 0; c < 2; ++c) {
+                for (int c = 0; c < 2; ++c)
 #pragma unroll
                     for (int g = 4; g < 32; g *= 2) l[t][c] += __shfl_xor_sync(0xffffffffu, l[t][c], g);
-                    if (lane < 4) ml_of[kw][head_of_warp + t * 8 + 2 * lane + c] = make_float2(m[t][c], l[t][c]);
-                }
-            mbar_arrive_warp(join_bar[0]);
-            if (!mbar_wait(join_bar[0], joins & 1u, abort_p, limit)) break;
+            if (!wait(B_JEMPTY, unit ^ 1u)) break;
 #pragma unroll
             for (int t = 0; t < kNT; ++t)
 #pragma unroll
                 for (int c = 0; c < 2; ++c) {
-                    const int row = head_of_warp + t * 8 + 2 * (lane & 3) + c;
-                    if (row >= q_rows) continue;
-                    float top = neg_inf();
-#pragma unroll
-                    for (int w = 0; w < kKeyWarps; ++w) top = fmaxf(top, ml_of[w][row].x);
-                    const float f = m[t][c] == neg_inf() ? 0.f : ex2_approx(m[t][c] - top);
-                    float* dst = join + (kw * S::kRows + row) * S::kJoinStride + key_of_lane;
+                    const int row = t * 8 + 2 * (lane & 3) + c;
+                    if (first_row + row >= p.group) continue;       // padding
+                    if (lane < 4) s_ml[warp][row] = make_float2(m[t][c], l[t][c]);
+                    float* dst = join + (warp * S::kWarpRows + row) * S::kJoinStride + key_of_lane;
 #pragma unroll
                     for (int j = 0; j < D_V / 16; ++j) {
-                        dst[16 * j] = o[j][t][c] * f;
-                        dst[16 * j + 8] = o[j][t][c + 2] * f;
+                        dst[16 * j] = o[j][t][c];
+                        dst[16 * j + 8] = o[j][t][c + 2];
                     }
                 }
-            mbar_arrive_warp(join_bar[1]);
-            if (!mbar_wait(join_bar[1], joins & 1u, abort_p, limit)) break;
-            ++joins;
-            const int64_t slot = 2 * static_cast<int64_t>(blockIdx.x) + (d.flags & FLAG_SECOND_SLOT ? 1 : 0);
-            for (int e = warp; e < q_rows; e += S::kConsumers) {
+            mbar_arrive_warp(bar(B_JFULL));
+            if (!wait(B_JFULL, unit)) break;
+            // ---------------------------------------------------------------- the warps that share a head, joined; a row per warp
+            const int32_t head0 = p.first_head(of.unit), rows = p.rows_of(of.unit);
+            for (int32_t e = warp; e < rows; e += S::kConsumers) {
+                const int32_t head = e / p.group, in_group = e - head * p.group, r = in_group % S::kWarpRows;
+                const int warp0 = (S::kHeadSets == 1 ? 0 : in_group / S::kWarpRows * kSlices) + (head << p.key_slices_log2);
+                float2 ml[S::kTurns * kSlices];
                 float top = neg_inf(), sum = 0.f;
                 float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll
-                for (int w = 0; w < kKeyWarps; ++w) top = fmaxf(top, ml_of[w][e].x);
+                for (int w = 0; w < S::kTurns * kSlices; ++w) {
+                    ml[w] = w % kSlices < key_slices ? s_ml[warp0 + w][r] : make_float2(neg_inf(), 0.f);
+                    top = fmaxf(top, ml[w].x);
+                }
+                const float ref = top == neg_inf() ? 0.f : top;
 #pragma unroll
-                for (int w = 0; w < kKeyWarps; ++w) {
-                    const float2 ml = ml_of[w][e];
-                    if (ml.x != neg_inf()) sum += ml.y * ex2_approx(ml.x - top);
-                    const float4 x = *reinterpret_cast<const float4*>(join + (w * S::kRows + e) * S::kJoinStride + 4 * lane);
-                    acc.x += x.x; acc.y += x.y; acc.z += x.z; acc.w += x.w;
+                for (int w = 0; w < S::kTurns * kSlices; ++w) {
+                    if (w % kSlices >= key_slices) continue;
+                    const float f = ex2_approx(ml[w].x - ref);
+                    const float4 x = *reinterpret_cast<const float4*>(join + ((warp0 + w) * S::kWarpRows + r) * S::kJoinStride + 4 * lane);
+                    sum += f * ml[w].y;
+                    acc.x += f * x.x; acc.y += f * x.y; acc.z += f * x.z; acc.w += f * x.w;
                 }
                 const float inv = top == neg_inf() ? 0.f : 1.f / sum, lse2 = top == neg_inf() ? top : top + log2f(sum);
                 acc.x *= inv; acc.y *= inv; acc.z *= inv; acc.w *= inv;
-                if (d.flags & FLAG_PARTIAL) {
-                    reinterpret_cast<float4*>(p.part_o + (slot * S::kRows + e) * D_V)[lane] = acc;
-                    if (lane == 0) p.part_lse2[slot * S::kRows + e] = lse2;
+                if (of.slot >= 0) {
+                    const int64_t row = static_cast<int64_t>(of.slot) * p.unit_rows + e;
+                    reinterpret_cast<float4*>(p.part_o + row * D_V)[lane] = acc;
+                    if (lane == 0) p.part_lse2[row] = lse2;
                 } else {
-                    reinterpret_cast<uint2*>(p.out + (static_cast<int64_t>(b) * p.h + head0 + e) * D_V)[lane] =
+                    reinterpret_cast<uint2*>(p.out + (static_cast<int64_t>(of.seq) * p.h + head0 + e) * D_V)[lane] =
                         make_uint2(pack_bf16x2(acc.x, acc.y), pack_bf16x2(acc.z, acc.w));
-                    if (lane == 0) p.lse[static_cast<int64_t>(head0 + e) * p.n_seqs + b] = lse2 * 0.6931471805599453f;
+                    if (lane == 0) p.lse[static_cast<int64_t>(head0 + e) * p.n_seqs + of.seq] = lse2 * 0.6931471805599453f;
                 }
             }
+            mbar_arrive_warp(bar(B_JEMPTY));
         }
     }
     __syncthreads();
@@ -435,128 +657,135 @@ hydra_decode_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_cons
     }
 }
 
-// Rows (sequence, query head) whose keys several thread blocks had: (O, LSE) of the parts joined in the order of the keys.
-// Rows without a key: O = 0, LSE = -inf. The others have been written. kWarps per row.
-constexpr int kJoinThreads = 256;
-template <int kWarps>
-__global__ void __launch_bounds__(kJoinThreads)
-hydra_decode_join_kernel(const DecodeParams p, int32_t n_blocks_max)
+struct DecodeJoin {
+    int32_t item;                           // sequence * units of a sequence + unit of the sequence
+    int32_t piece, parts;                   // the first piece with tiles of it, and how many there are (0: nothing to join)
+};
+
+// (O, LSE) of the parts of cut units, joined in the order of the keys. Part i of a unit is the beginning of piece c0 + i, but the
+// first the end of its piece. A thread block per piece: those whose piece goes on with a unit share its rows. A row of up to
+// eight parts has a warp, of up to 32 a block; of more, every 32 have a block that puts their join in the place of the first, and
+// the block that comes last joins those. The blocks are small enough to stand beside those of the kernel before, and find out
+// what they have to do while that one still runs.
+__global__ void __launch_bounds__(32 * kJoinWarps, 9)
+hydra_decode_join_kernel(const DecodeParams p)
 {
-    constexpr int kRowsPerBlock = kJoinThreads / 32 / kWarps;
-    __shared__ float4 s_acc[kWarps > 1 ? kWarps : 1][32];
-    __shared__ float s_sum[kWarps > 1 ? kWarps : 1];
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, w = warp % kWarps;
-    const int64_t row = static_cast<int64_t>(blockIdx.x) * kRowsPerBlock + warp / kWarps;
-    const bool valid = row < static_cast<int64_t>(p.n_seqs) * p.h;
-    const int32_t b = valid ? static_cast<int32_t>(row / p.h) : 0, a = valid ? static_cast<int32_t>(row - static_cast<int64_t>(b) * p.h) : 0;
-    const int32_t per_seq = p.kv_heads * p.chunks;
-    int64_t before = 0, all = 0;
-    for (int32_t i = lane; i < p.n_seqs; i += 32) {
-        const int32_t n = tiles_of(p, seq_len_of(p, i));
-        all += n;
-        if (i < b) before += n;
+    __shared__ float4 s_o[kJoinWarps][32];
+    __shared__ float s_lse2[kJoinWarps];
+    __shared__ int32_t s_last;
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    __shared__ DecodeJoin s_join;
+    if (warp == 0) {                                    // the unit that this block's piece went on with
+        const Lengths lengths(p, lane);
+        const Pieces pieces(p, lengths.total);
+        DecodeJoin join{0, 0, 0};
+        int32_t lo = 0, hi = 0;
+        if (static_cast<int32_t>(blockIdx.x) < pieces.count()) pieces.range(blockIdx.x, lo, hi);
+        if (lo < hi) {
+            int32_t b, before, len;
+            lengths.find(p, lane, p.by_units(lo), b, len, before);
+            const int32_t n_tiles = tiles_of(p, len), in_seq = lo - before * p.units, unit = in_seq / n_tiles, tile = in_seq - unit * n_tiles;
+            if (tile > 0) {
+                join.item = b * p.units + unit;
+                join.piece = pieces.piece_of(lo - tile);
+                join.parts = pieces.piece_of(lo - tile + n_tiles - 1) - join.piece + 1;
+            }
+        }
+        if (lane == 0) s_join = join;
     }
-#pragma unroll
-    for (int d = 16; d > 0; d /= 2) {
-        all += __shfl_xor_sync(0xffffffffu, all, d);
-        before += __shfl_xor_sync(0xffffffffu, before, d);
-    }
-    const int32_t n_tiles = tiles_of(p, seq_len_of(p, b));
-    const int32_t kvh = a / p.group, in_group = a - kvh * p.group, chunk = in_group / p.chunk_rows, r = in_group - chunk * p.chunk_rows;
-    const int64_t total = all * per_seq, n_blocks = min(static_cast<int64_t>(n_blocks_max), total);
-    const int64_t t0 = before * per_seq + static_cast<int64_t>(kvh * p.chunks + chunk) * n_tiles;
-    const int64_t c0 = n_tiles ? block_of(total, t0, n_blocks) : 0, c1 = n_tiles ? block_of(total, t0 + n_tiles - 1, n_blocks) : 0;
-    uint2* const out = reinterpret_cast<uint2*>(p.out + row * D_V) + lane;
-    float* const lse = p.lse + static_cast<int64_t>(a) * p.n_seqs + b;
+    __syncthreads();
+    const DecodeJoin join = s_join;
+    const int32_t b = join.item / p.units, unit = join.item - b * p.units;
     wait_for_previous_launch();
-    if (!valid || (n_tiles > 0 && c0 == c1)) return;    // (all warps of a row leave together)
-    if (n_tiles == 0) {
-        if (w == 0) {
-            *out = make_uint2(0u, 0u);
-            if (lane == 0) *lse = neg_inf();
-        }
-        return;
-    }
-    const int32_t parts = static_cast<int32_t>(c1 - c0) + 1;
-    // part i is the beginning of block c0 + i's run, but the first is the end of its block's
-    auto at = [&](int32_t i) { return (2 * (c0 + i) + (i == 0 ? 1 : 0)) * p.chunk_rows + r; };
-    float top = neg_inf();
-    for (int32_t i = lane; i < parts; i += 32) top = fmaxf(top, __ldcg(p.part_lse2 + at(i)));
+    if (join.parts == 0) return;
+    const int32_t rows = p.rows_of(unit), parts = join.parts, chunks = (parts + kJoinChunk - 1) / kJoinChunk;
+    const bool by_warp = parts <= kJoinParts;
+
+    // the join of parts first, first + step, ... (count of them, at most kJoinParts)
+    auto join_parts = [&](int32_t r, int32_t first, int32_t step, int32_t count) -> Joined {
+        float part[kJoinParts];
+        float4 x[kJoinParts];
 #pragma unroll
-    for (int d = 16; d > 0; d /= 2) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, d));
-    const float ref = top == neg_inf() ? 0.f : top;
-    float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
-    float sum = 0.f;
-#pragma unroll 4
-    for (int32_t i = w; i < parts; i += kWarps) {
-        const float f = ex2_approx(__ldcg(p.part_lse2 + at(i)) - ref);
-        const float4 x = __ldcg(reinterpret_cast<const float4*>(p.part_o + at(i) * D_V) + lane);
-        sum += f;
-        acc.x += f * x.x; acc.y += f * x.y; acc.z += f * x.z; acc.w += f * x.w;
-    }
-    if (kWarps > 1) {
-        s_acc[w][lane] = acc;
-        if (lane == 0) s_sum[w] = sum;
-        __syncthreads();
-        if (w) return;
-        for (int i = 1; i < kWarps; ++i) {
-            const float4 x = s_acc[i][lane];
-            acc.x += x.x; acc.y += x.y; acc.z += x.z; acc.w += x.w;
-            sum += s_sum[i];
+        for (int j = 0; j < kJoinParts; ++j) {
+            const int32_t i = first + j * step, at = (2 * (join.piece + i) + (i == 0 ? 1 : 0)) * p.unit_rows + r;
+            part[j] = j < count ? __ldcg(p.part_lse2 + at) : neg_inf();
+            x[j] = j < count ? __ldcg(reinterpret_cast<const float4*>(p.part_o + static_cast<int64_t>(at) * D_V) + lane) : make_float4(0.f, 0.f, 0.f, 0.f);
         }
+        return join_of(part, x);
+    };
+    auto write = [&](int32_t r, const Joined& v) {
+        const int32_t a = p.first_head(unit) + r;
+        reinterpret_cast<uint2*>(p.out + (static_cast<int64_t>(b) * p.h + a) * D_V)[lane] =
+            make_uint2(pack_bf16x2(v.o.x, v.o.y), pack_bf16x2(v.o.z, v.o.w));
+        if (lane == 0) p.lse[static_cast<int64_t>(a) * p.n_seqs + b] = v.lse2 * 0.6931471805599453f;
+    };
+    // warp w's share of a row's parts first + step * [0, count)
+    auto join_block = [&](int32_t r, int32_t first, int32_t step, int32_t count) -> Joined {
+        const int32_t mine = count > warp ? (count - warp + kJoinWarps - 1) / kJoinWarps : 0;
+        __syncthreads();                                // (what the block joined before has been read)
+        const Joined v = join_parts(r, first + warp * step, step * kJoinWarps, mine);
+        s_o[warp][lane] = v.o;
+        if (lane == 0) s_lse2[warp] = v.lse2;
+        __syncthreads();
+        float part[kJoinWarps];
+        float4 x[kJoinWarps];
+#pragma unroll
+        for (int w = 0; w < kJoinWarps; ++w) { part[w] = s_lse2[w]; x[w] = s_o[w][lane]; }
+        return join_of(part, x);
+    };
+
+    const int32_t helpers = parts - 1, tasks = by_warp ? (rows + kJoinWarps - 1) / kJoinWarps : rows * chunks;
+    for (int32_t task = static_cast<int32_t>(blockIdx.x) - join.piece - 1; task < tasks; task += helpers) {
+        if (by_warp) {
+            const int32_t r = task * kJoinWarps + warp;
+            if (r < rows) write(r, join_parts(r, 0, 1, parts));
+            continue;
+        }
+        const int32_t r = task / chunks, first = (task - r * chunks) * kJoinChunk;
+        Joined v = join_block(r, first, 1, min(kJoinChunk, parts - first));
+        if (chunks > 1) {
+            if (warp == 0) {
+                const int32_t at = (2 * (join.piece + first) + (first == 0 ? 1 : 0)) * p.unit_rows + r;
+                reinterpret_cast<float4*>(p.part_o + static_cast<int64_t>(at) * D_V)[lane] = v.o;
+                if (lane == 0) p.part_lse2[at] = v.lse2;
+                __threadfence();
+                __syncwarp();
+                if (lane == 0) s_last = atomicAdd(p.arrived + join.piece + 1 + r, 1) == chunks - 1;
+            }
+            __syncthreads();
+            if (!s_last) continue;
+            __threadfence();
+            v = join_block(r, 0, kJoinChunk, chunks);   // (at most 24 of them)
+        }
+        if (warp == 0) write(r, v);
     }
-    const float inv = top == neg_inf() ? 0.f : 1.f / sum;
-    *out = make_uint2(pack_bf16x2(acc.x * inv, acc.y * inv), pack_bf16x2(acc.z * inv, acc.w * inv));
-    if (lane == 0) *lse = top == neg_inf() ? top : (top + log2f(sum)) * 0.6931471805599453f;
 }
 
-struct Form {
-    int32_t rows, tile_keys, per_sm;
-    cudaError_t (*launch)(const CUtensorMap&, const CUtensorMap&, const DecodeParams&, uint64_t, int, cudaStream_t);
-};
+using LaunchFn = cudaError_t (*)(const CUtensorMap (&)[4], const DecodeParams&, uint64_t, cudaStream_t);
 template <class S>
-cudaError_t launch_one(const CUtensorMap& mk, const CUtensorMap& mv, const DecodeParams& p, uint64_t call_tag, int grid,
-                       cudaStream_t stream)
+cudaError_t launch_one(const CUtensorMap (&maps)[4], const DecodeParams& p, uint64_t call_tag, cudaStream_t stream)
 {
     static OncePerDevice configured;
     const auto kernel = hydra_decode_kernel<S>;
     if (cudaError_t e = allow_dynamic_smem(kernel, S::kSmem, configured)) return e;
-    return launch_overlapped(kernel, grid, S::kThreads, S::kSmem, stream, mk, mv, p, call_tag);
+    return launch_overlapped(kernel, p.blocks, S::kThreads, S::kSmem, stream, maps[0], maps[1], maps[2], maps[3], p, call_tag);
 }
-template <class S>
-constexpr Form form_of() { return {S::kRows, S::kKeys, S::kPerSm, launch_one<S>}; }
-
-// by query heads per K / V head
 template <int kDqk>
-const Form& form_for(int32_t group)
+LaunchFn form_for(int32_t group)
 {
-    static constexpr Form one = form_of<Shape<kDqk, 1, 1, 4, 2>>(), two = form_of<Shape<kDqk, 2, 1, 2, 3>>(),
-                          four = form_of<Shape<kDqk, 2, 2, 4, 1>>();
-    return group <= 8 ? one : group <= 16 ? two : four;
+    return group <= 8 ? launch_one<Shape<kDqk, 1, 1>> : group <= 16 ? launch_one<Shape<kDqk, 1, 2>> : launch_one<Shape<kDqk, 2, 2>>;
 }
-const Form& form_for(int32_t d_qk, int32_t group) { return d_qk == 192 ? form_for<192>(group) : form_for<128>(group); }
 
 }  // namespace
 
-DecodeForm decode_form(int32_t d_qk, int32_t group)
+cudaError_t launch_decode(const CUtensorMap (&maps)[4], const DecodeParams& p, int32_t d_qk, uint64_t call_tag, cudaStream_t stream)
 {
-    const Form& f = form_for(d_qk, group);
-    return {f.rows, f.tile_keys, f.per_sm};
+    return (d_qk == 192 ? form_for<192>(p.group) : form_for<128>(p.group))(maps, p, call_tag, stream);
 }
 
-cudaError_t launch_decode(const CUtensorMap& mk, const CUtensorMap& mv, const DecodeParams& p, int32_t d_qk, uint64_t call_tag,
-                          int grid, cudaStream_t stream)
+cudaError_t launch_decode_join(const DecodeParams& p, cudaStream_t stream)
 {
-    return form_for(d_qk, p.group).launch(mk, mv, p, call_tag, grid, stream);
-}
-
-cudaError_t launch_decode_join(const DecodeParams& p, int grid_of_parts, cudaStream_t stream)
-{
-    const int64_t rows = static_cast<int64_t>(p.n_seqs) * p.h;
-    // few pairs have many parts each: eight warps share a row
-    if (static_cast<int64_t>(p.n_seqs) * p.kv_heads * p.chunks < grid_of_parts / 4)
-        return launch_overlapped(hydra_decode_join_kernel<8>, static_cast<int>(rows), kJoinThreads, 0, stream, p, grid_of_parts);
-    return launch_overlapped(hydra_decode_join_kernel<1>, static_cast<int>((rows + 7) / 8), kJoinThreads, 0, stream, p, grid_of_parts);
+    return launch_overlapped(hydra_decode_join_kernel, DECODE_LEVELS * p.blocks, 32 * kJoinWarps, 0, stream, p);
 }
 
 }  // namespace hydra

@@ -14,7 +14,8 @@ constexpr int D_V = HYDRA_D_V;
 constexpr int TILE = 128;       // rows of a q tile and of a kv tile
 constexpr int SUB = 64;         // rows of a q sub-tile in the key-side backward kernel
 constexpr int FWD_SHORT_KEYS = 64;   // keys per step of the short-sequence forward kernel
-constexpr int DECODE_MAX_BLOCKS = 4 * 148;   // thread blocks of the attention over a paged cache
+constexpr int DECODE_MAX_BLOCKS = 148;   // thread blocks of the attention over a paged cache
+constexpr int DECODE_LEVELS = 5;         // pieces that a block's share of its work is cut into, at most
 
 // One (q-chunk, kv-chunk) pair with absolute token offsets, as the kernels see it.
 struct PairDev {
@@ -136,6 +137,7 @@ struct StatusBlock {
     // producer thread of CTA 0 between its first and its last instruction (same index as next_item)
     uint64_t probe_cycles[4];
     uint64_t probe_ns[4];
+    uint64_t pieces;            // attention over a paged cache: pieces of work popped so far, below the call's number
 };
 enum : int { QUEUE_FWD = 0, QUEUE_DKV = 1, QUEUE_DQ = 2, QUEUE_FWD_SHORT = 3 };
 
@@ -294,21 +296,59 @@ struct MergeParams {
     int32_t split;              // thread blocks that share an item (set by launch_merge)
 };
 
+// n / d for 0 <= n <= 2^30 and 1 <= d <= 2^30, by a multiplication: with 2^(s-1) < d <= 2^s and m = ceil(2^(31+s) / d) < 2^32, n m
+// exceeds n 2^(31+s) / d by less than n < 2^(31+s) / d (n d <= 2^(30+s)), so the quotient's whole part is the same. (m = 0
+// stands for d = 1.)
+struct DivKeys {
+    uint32_t m, shift;
+    static DivKeys by(uint32_t d)
+    {
+        if (d == 1) return {0u, 0u};
+        uint32_t s = 1;
+        while ((1u << s) < d) ++s;
+        return {static_cast<uint32_t>(((uint64_t{1} << (31 + s)) + d - 1) / d), s - 1};
+    }
+#ifdef __CUDACC__
+    __device__ __forceinline__ int32_t operator()(int32_t n) const { return m ? static_cast<int32_t>(__umulhi(static_cast<uint32_t>(n), m) >> shift) : n; }
+#endif
+};
 struct DecodeParams {
     const uint16_t* q;          // bf16 [n_seqs, h, d_qk], rows of a sequence q_stride elements apart
     int64_t q_stride;
     const int32_t* page_table;  // [n_seqs, max_pages]
     const int32_t* seq_lens;    // [n_seqs]
     uint16_t* out; float* lse;  // bf16 [n_seqs, h, d_v]; [h, n_seqs]
-    // (O, log2 of the sum of 2^score) of pairs cut between thread blocks: two slots per block, a row per query head
+    // (O, log2 of the sum of 2^score) of pairs cut between pieces: two slots per piece, a row per query head
     float* part_o; float* part_lse2;
+    int32_t* arrived;           // one per piece: a counter for the join
     int32_t n_seqs, max_pages, page_size, n_pages;
     int32_t max_len;            // tokens that a row of the page table holds
-    int32_t box_rows;           // rows of a TMA box: a divisor of page_size
-    int32_t h, kv_heads;
+    int32_t box_rows, boxes;    // keys of a TMA box: a divisor of page_size; boxes of a tile
+    DivKeys by_page;
+    int32_t h;
     int32_t group;              // query heads per K / V head
-    int32_t chunks, chunk_rows; // thread blocks' shares of a group, chunk_rows query heads each
-    int32_t tile_keys;          // keys of a tile
+    // A unit of work: unit_kv_heads K / V heads with their query heads; or, with more than 32 query heads per K / V head, one K / V
+    // head with 32 of them (chunks units per head). A tile is 64 rows: 16 << key_slices_log2 keys of each of a unit's heads.
+    int32_t units;              // of a sequence
+    int32_t blocks;             // thread blocks
+    DivKeys by_units, by_blocks;
+    int32_t unit_kv_heads, unit_rows, chunks;
+    int32_t key_slices_log2, tile_keys, tile_shift;
+#ifdef __CUDACC__
+    __device__ __forceinline__ int32_t first_kv_head(int32_t unit) const { return chunks == 1 ? unit * unit_kv_heads : unit / chunks; }
+    __device__ __forceinline__ int32_t first_head(int32_t unit) const
+    {
+        return chunks == 1 ? unit * unit_rows : unit / chunks * group + unit % chunks * unit_rows;
+    }
+    __device__ __forceinline__ int32_t rows_of(int32_t unit) const
+    {
+        return chunks == 1 ? unit_rows : min(unit_rows, group - unit % chunks * unit_rows);
+    }
+    __device__ __forceinline__ int32_t unit_of(int32_t head) const
+    {
+        return chunks == 1 ? head / unit_rows : head / group * chunks + head % group / unit_rows;
+    }
+#endif
     float scale_log2;           // softmax_scale * log2(e)
     StatusBlock* status;
     uint64_t wait_limit_ns;
@@ -362,13 +402,9 @@ cudaError_t launch_gate(const void* out, const void* gate, void* y, int64_t n8, 
 cudaError_t launch_gate_bwd(const void* dy, const void* out, const void* gate, void* d_out, void* d_gate, int64_t n8,
                             cudaStream_t stream);
 // attention of one new token over a paged cache, and the join of what thread blocks had of one pair (decode_kernel.cu)
-struct DecodeForm {
-    int32_t chunk_rows, tile_keys, per_sm;      // query heads of a thread block, keys of a tile, thread blocks per SM
-};
-DecodeForm decode_form(int32_t d_qk, int32_t group);
-cudaError_t launch_decode(const CUtensorMap& mk, const CUtensorMap& mv, const DecodeParams& p, int32_t d_qk, uint64_t call_tag,
-                          int grid, cudaStream_t stream);
-cudaError_t launch_decode_join(const DecodeParams& p, int decode_grid, cudaStream_t stream);
+// maps: boxes of K and V of p.box_rows keys of a unit's heads, and of eight of one head
+cudaError_t launch_decode(const CUtensorMap (&maps)[4], const DecodeParams& p, int32_t d_qk, uint64_t call_tag, cudaStream_t stream);
+cudaError_t launch_decode_join(const DecodeParams& p, cudaStream_t stream);
 // rotary positions with several axes; new keys and values into a paged cache (pe: MLA form, k is the up-projection)
 // (paged_ops.cu)
 cudaError_t launch_rope_axes(const void* x, int64_t x_stride, const int32_t* positions, int64_t n_tokens, int32_t n_heads,

@@ -103,8 +103,8 @@ def decode(q=A, c=None, h=4, scale=0.1, out=A, lse=A, ws=A, nbytes=1 << 30, qs=N
     (dict(h=0), INVALID), (dict(h=3), INVALID), (dict(scale=0.0), INVALID), (dict(scale=float("nan")), INVALID),
     (dict(scale=float("inf")), INVALID), (dict(qs=760), INVALID), (dict(qs=772), UNSUPPORTED), (dict(c=cache(d_qk=64)), UNSUPPORTED),
     (dict(c=cache(d_v=64)), UNSUPPORTED), (dict(c=cache(page_size=12)), UNSUPPORTED), (dict(c=cache(page_size=4)), UNSUPPORTED),
-    (dict(c=cache(n_pages=2**30)), UNSUPPORTED), (dict(c=cache(n_pages=2**25, n_kv_heads=2, page_size=32)), UNSUPPORTED),
-    (dict(c=cache(n_seqs=2**30)), UNSUPPORTED), (dict(q=None), INVALID), (dict(q=A + 8), INVALID), (dict(out=None), INVALID),
+    (dict(c=cache(n_seqs=2**30)), UNSUPPORTED), (dict(c=cache(max_pages=2**27)), UNSUPPORTED),
+    (dict(c=cache(n_seqs=2**13, max_pages=2**18)), UNSUPPORTED), (dict(q=None), INVALID), (dict(q=A + 8), INVALID), (dict(out=None), INVALID),
     (dict(lse=None), INVALID), (dict(out=A + 8), INVALID), (dict(ws=None), INVALID), (dict(ws=A + 8), INVALID),
     (dict(nbytes=P.hydra_workspace_bytes_decode(4, 2) - 1), P.HYDRA_ERR_WORKSPACE_TOO_SMALL)])
 def test_attn_decode(change, status):
