@@ -173,15 +173,16 @@ struct Lengths {
     }
 };
 
-// How the tiles of a call are cut: into equal shares, one per thread block, and a share of 32 tiles or more into pieces of 7/8,
-// 1/16, 1/32, 1/64 and 1/64 of it, which are run in that order: the first pieces of all shares, then the second ones, ... Pieces are
-// numbered in the order of their tiles.
+// How the tiles of a call are cut: into equal shares, one per thread block, and a share of 64 tiles or more into pieces of 7/8,
+// 1/16, 1/32, 1/64 and 1/64 of it (of 32 or more, of 7/8, 1/16, 1/32 and 1/32), which are run in that order: the first pieces of all
+// shares, then the second ones, ... Pieces are numbered in the order of their tiles; none in front of the last tile is empty, for
+// a unit's parts are counted by them.
 struct Pieces {
     int32_t total, blocks, share, levels, start[DECODE_LEVELS + 1];
     __device__ __forceinline__ Pieces(const DecodeParams& p, int32_t tiles_of_a_unit)
         : total(tiles_of_a_unit * p.units), blocks(p.blocks), share(p.by_blocks(total + p.blocks - 1))
     {
-        levels = share < 32 ? 1 : DECODE_LEVELS;
+        levels = share < 32 ? 1 : share < 64 ? DECODE_LEVELS - 1 : DECODE_LEVELS;
         start[0] = 0;
 #pragma unroll
         for (int l = 1; l <= DECODE_LEVELS; ++l) start[l] = share - (l < levels ? share >> (l + 2) : 0);
@@ -301,6 +302,9 @@ hydra_decode_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_cons
     const uint64_t limit = p.wait_limit_ns;
     volatile int* abort_p = &abort_flag;
     auto wait = [&](int i, uint32_t parity) { return mbar_wait(bar(i), parity & 1u, abort_p, limit); };
+    // Lanes that have seen a phase end at different polls have to come together again: the next matrix load or product wants the
+    // whole warp.
+    auto wait_together = [&](int i, uint32_t parity) { return __all_sync(0xffffffffu, wait(i, parity)) != 0; };
 
     if (warp == S::kConsumers) {
         // ------------------------------------------------------------------ pieces, page table, q
@@ -481,13 +485,13 @@ hydra_decode_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_cons
         uint32_t unit = kEnd;
         for (uint32_t n = 0;; ++n) {
             const int st = static_cast<int>(n % S::kStages);
-            if (!wait(B_FULL + st, n / S::kStages)) break;
+            if (!wait_together(B_FULL + st, n / S::kStages)) break;
             const TileDesc d = s_tile[st];
             if (d.unit == kEnd) break;
             if ((d.unit & ~kLastOfUnit) != unit) {
                 unit = d.unit & ~kLastOfUnit;
                 const int q_slot = static_cast<int>(unit % S::kQSlots);
-                if (!wait(B_QFULL + q_slot, unit / S::kQSlots)) break;
+                if (!wait_together(B_QFULL + q_slot, unit / S::kQSlots)) break;
                 of = s_unit[q_slot];
 #pragma unroll
                 for (int t = 0; t < kNT; ++t) {
@@ -500,6 +504,9 @@ hydra_decode_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_cons
                         q[ks][t][0] = f[0]; q[ks][t][1] = f[1]; q[ks + 1][t][0] = f[2]; q[ks + 1][t][1] = f[3];
                     }
                 }
+                // Nothing has used the loaded rows yet. Without the fence an asynchronous copy of the slot's next unit can be ahead of
+                // the last of these loads, as one of the units of one tile or two was in some ten calls of a share of 32.
+                fence_proxy_async_smem();
                 mbar_arrive_warp(bar(B_QEMPTY + q_slot));
 #pragma unroll
                 for (int i = 0; i < D_V / 16 * kNT * 4; ++i) o[i / (4 * kNT)][i / 4 % kNT][i % 4] = 0.f;
@@ -589,7 +596,7 @@ hydra_decode_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_cons
                 for (int c = 0; c < 2; ++c)
 #pragma unroll
                     for (int g = 4; g < 32; g *= 2) l[t][c] += __shfl_xor_sync(0xffffffffu, l[t][c], g);
-            if (!wait(B_JEMPTY, unit ^ 1u)) break;
+            if (!wait_together(B_JEMPTY, unit ^ 1u)) break;
 #pragma unroll
             for (int t = 0; t < kNT; ++t)
 #pragma unroll
@@ -605,7 +612,7 @@ hydra_decode_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_cons
                     }
                 }
             mbar_arrive_warp(bar(B_JFULL));
-            if (!wait(B_JFULL, unit)) break;
+            if (!wait_together(B_JFULL, unit)) break;
             // ---------------------------------------------------------------- the warps that share a head, joined; a row per warp
             const int32_t head0 = p.first_head(of.unit), rows = p.rows_of(of.unit);
             for (int32_t e = warp; e < rows; e += S::kConsumers) {

@@ -85,6 +85,27 @@ def test_pairs_cut_between_thread_blocks(lengths, h, hk):
     solve(lengths, h, hk, 192, 64, seed=sum(lengths))
 
 
+@pytest.mark.parametrize("share,rest,h,hk", [(31, 100, 4, 4), (32, 0, 4, 4), (33, 7, 1, 1), (63, 40, 2, 2), (64, 0, 8, 4), (65, 147, 1, 1), (130, 1, 2, 2)])
+def test_shares_that_are_run_in_pieces(share, rest, h, hk):
+    """Long enough for every thread block's share of the tiles to be cut and its last pieces popped, at the shares where the number of
+    pieces changes; call after call on two problems in turn, every result bit for bit the first one."""
+    tile = 64 // hk                                 # keys; one unit per sequence, 148 shares of `share` tiles
+    tiles = 148 * share - rest
+    lengths = [tile * (tiles // 2) - 3, 5, tile * (tiles // 3), 0, tile * 7 + 1]
+    lengths.append(tile * (tiles - sum(-(-n // tile) for n in lengths)) - tile // 2)
+    p = Problem(lengths, h, hk, 128, 64, seed=share, garbage=False)
+    other = Problem([n // 2 for n in lengths], h, hk, 128, 64, seed=share + 1, garbage=False)
+    p.run()
+    p.verify()
+    first, first_l = p.out.clone(), p.lse.clone()
+    for _ in range(10):
+        other.run()
+        p.out.fill_(float("nan"))
+        p.run()
+        assert torch.equal(p.out, first) and torch.equal(p.lse, first_l)
+    other.verify()
+
+
 def test_missing_pages_and_lengths_outside_the_table():
     def table(t, n):
         t[0, 1] = -1                                # in the middle
