@@ -697,15 +697,17 @@ def _rows(x, stride: Optional[int]) -> Tuple[Optional[int], int]:
     """(device pointer, elements between tokens) of rows that are contiguous but for the distance between tokens: a tensor
     [tokens, ...], possibly a slice of a wider one, or a raw pointer with its stride."""
     if x is None or isinstance(x, int):
-        return x, 0 if stride is None else int(stride)
-    want = 1
-    for size, step in zip(reversed(x.shape[1:]), reversed(x.stride()[1:])):
-        if size != 1 and step != want:
-            raise ValueError("a token's rows must be contiguous")
-        want *= size
+        return x, 0 if stride is None else stride
     if not x.is_cuda:
         raise ValueError("tensors must be CUDA tensors")
-    return x.data_ptr(), int(stride) if stride is not None else x.stride(0) if x.shape[0] > 1 else max(want, x.stride(0))
+    steps = x.stride()
+    if not x.is_contiguous():
+        want = 1
+        for size, step in zip(x.shape[:0:-1], steps[:0:-1]):
+            if size != 1 and step != want:
+                raise ValueError("a token's rows must be contiguous")
+            want *= size
+    return x.data_ptr(), steps[0] if stride is None else stride
 
 
 def _spec(x) -> Optional[int]:
