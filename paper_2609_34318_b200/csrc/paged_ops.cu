@@ -43,7 +43,8 @@ struct PlaceParams {
     // the cache
     const int32_t *page_table, *seq_lens, *cu_new;
     int32_t n_seqs, max_pages, page_size, n_pages, heads;
-    // a warp's share: `tokens` tokens, or 1 / splits of the heads of one; vectors of a token's share in k, in v, and its rotary ones
+    // a warp's share: `tokens` tokens, or share_heads heads (the last of the splits: what is left) of one; vectors of a token's share in
+    // k, in v, and its rotary ones
     int32_t tokens, splits, share_heads;
     Div by_k_token, by_k_row, by_v_token, by_v_row, by_rot_token, by_rot_row;
 };
@@ -82,7 +83,7 @@ hydra_place_rows_kernel(const PlaceParams p)
         const int64_t t0 = share / p.splits * p.tokens;
         const int32_t head0 = static_cast<int32_t>(share % p.splits) * p.share_heads;
         const uint32_t n_tok = static_cast<uint32_t>(min(static_cast<int64_t>(p.tokens), p.n_tokens - t0));
-        const uint32_t n_k = n_tok * p.by_k_token.d;
+        const uint32_t n_heads = static_cast<uint32_t>(min(p.share_heads, p.heads - head0)), n_k = n_tok * n_heads * p.k_vecs;
         const int64_t k_from = t0 * p.k_stride + static_cast<int64_t>(head0) * p.k_vecs;
         // rows of k, in the order in which they lie there
         auto load_k = [&](uint32_t e) {
@@ -207,7 +208,7 @@ hydra_place_rows_kernel(const PlaceParams p)
                 if (const uint32_t e = e0 + 32 * u; e < n_k && rotary(e)) store_k(e, w[u]);
         }
         if (kMode == PLACE_KV) {                        // rows of v
-            const uint32_t n_v = n_tok * p.by_v_token.d;
+            const uint32_t n_v = n_tok * n_heads * p.v_vecs;
             for (uint32_t e0 = lane; e0 < n_v; e0 += 32 * kInFlight) {
                 Words<kWords> w[kInFlight];
 #pragma unroll
@@ -225,7 +226,7 @@ hydra_place_rows_kernel(const PlaceParams p)
             }
         }
         if (kMode == PLACE_MLA) {                       // the turned key, for every head
-            const uint32_t n_rot = n_tok * p.by_rot_token.d;
+            const uint32_t n_rot = n_tok * n_heads * p.rot_vecs;
             for (uint32_t e = lane; e < n_rot; e += 32) {
                 const uint32_t tok = p.by_rot_token(e), in = e - tok * p.by_rot_token.d, head = p.by_rot_row(in), c = in - head * p.rot_vecs;
                 const float* src = s_cos + tok * p.pairs + c * kWords;
@@ -253,9 +254,11 @@ PlaceParams place_params(int64_t n_tokens, int32_t n_heads, const hydra_rope_t* 
     tokens = std::max<int64_t>(tokens, 1);
     const int64_t steps = (n_tokens + tokens - 1) / tokens;
     int32_t splits = 1;
-    auto vectors = [&] { return tokens * (n_heads / splits) * per_head; };
-    while (n_heads % (2 * splits) == 0 && (vectors() > 2 * kVectors || (steps * splits < kWarps && vectors() > 64))) splits *= 2;
-    const int32_t share = n_heads / splits, k = k_elems / elems, v = v_elems / elems, rot = rot_elems / elems;
+    auto share_heads = [&] { return (n_heads + splits - 1) / splits; };
+    auto vectors = [&] { return tokens * share_heads() * per_head; };
+    while (tokens == 1 && 2 * splits <= n_heads && (vectors() > 2 * kVectors || (steps * splits < kWarps && vectors() > 64))) splits *= 2;
+    const int32_t share = share_heads(), k = k_elems / elems, v = v_elems / elems, rot = rot_elems / elems;
+    splits = (n_heads + share - 1) / share;
     PlaceParams p{nullptr, nullptr, nullptr, nullptr, nullptr, 0, 0, 0, 0, 0, 0, k, row_elems / elems, v, rot0_elems / elems, rot,
                   positions, n_tokens, pairs, 0, rope ? rope->n_axes : 0, {}, 0.0, nullptr, nullptr, nullptr, 0, 0, 1, 0, n_heads,
                   static_cast<int32_t>(tokens), splits, share, Div(share * k), Div(k), Div(share * v), Div(v), Div(share * rot), Div(rot)};

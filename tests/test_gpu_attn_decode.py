@@ -201,6 +201,30 @@ def test_a_captured_call_follows_lengths_and_table():
         p.verify()
 
 
+def test_captured_calls_that_share_a_workspace_and_run_in_pieces():
+    """The pieces are counted in the workspace: two recorded calls and one that is not use the same, one after the other."""
+    a, b = Problem([16 * 148 * 40, 700, 0], 4, 4, 128, 64, seed=30, garbage=False), Problem([9000, 16 * 148 * 33], 4, 4, 192, 16, seed=31, garbage=False)
+    b.ws, b.check_ws = a.ws, a.check_ws
+    wants, graphs = [], []
+    for p in (a, b):
+        p.run()
+        p.verify()
+        wants.append((p.out.clone(), p.lse.clone()))
+        graphs.append(torch.cuda.CUDAGraph())
+        with torch.cuda.graph(graphs[-1]):
+            p.run()
+    for i in range(10):
+        for p in (a, b):
+            p.out.fill_(float("nan"))
+        graphs[0].replay()
+        graphs[1].replay()
+        if i % 3 == 0:
+            a.run()
+        for p, (out, lse) in zip((a, b), wants):
+            assert torch.equal(p.out, out) and torch.equal(p.lse, lse)
+    a.verify()
+
+
 def test_refused_calls_launch_nothing():
     import paper_2609_34318_b200 as P
     p = Problem([10], 4, 2, 192, 16, seed=10)

@@ -119,6 +119,14 @@ def test_many_heads_share_a_token_and_many_tokens_a_block():
     solve([600] * 5, [1] * 5, 1, 16, 8, 8, [2, 2], seed=4)
 
 
+@pytest.mark.parametrize("h", [3, 5, 33, 515])
+def test_numbers_of_heads_that_do_not_halve(h):
+    """A token's heads are shared by warps, the last of which has fewer of them."""
+    solve([1, 2], [4, 0], h, 192, 128, 8, [16, 16], mla=True, seed=h)
+    solve([1, 2], [4, 0], h, 128, 128, 8, [32, 32], seed=h)
+    solve([1, 1], [7, 20], h, 256, 512, 8, [64], offset=64, one_each=True, seed=h)
+
+
 def test_positions_of_the_cache_by_default_and_sequences_found_among_many():
     rng = np.random.default_rng(5)
     new = rng.integers(0, 4, 1500).tolist()

@@ -51,6 +51,13 @@ def test_sections_offsets_and_sizes(T, h, d, offset, axis_pairs, in_place):
     solve(T, h, d, offset, axis_pairs, in_place=in_place, seed=T)
 
 
+@pytest.mark.parametrize("T,h,d,axis_pairs", [(1, 33, 192, [8, 12, 12]), (3, 5, 1024, [40, 40]), (2, 131, 128, [16, 24, 24]), (1, 4101, 1024, [64])])
+def test_numbers_of_heads_that_do_not_halve(T, h, d, axis_pairs):
+    """A token's heads are shared by warps, the last of which has fewer of them."""
+    solve(T, h, d, 0, axis_pairs, seed=h)
+    solve(T, h, d, min(8, d - 2 * sum(axis_pairs)), axis_pairs, seed=h, in_place=True, inverse=True)
+
+
 @pytest.mark.parametrize("inverse", [False, True])
 @pytest.mark.parametrize("xs,ys", [(400, 384), (384, 392), (1000, 456)])
 def test_rows_that_are_slices(xs, ys, inverse):
