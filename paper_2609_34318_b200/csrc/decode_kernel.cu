@@ -14,7 +14,7 @@
 // beginning of another. Whole units are written straight to out / lse; cut ones leave (O, LSE) in fp32 in the workspace, and
 // hydra_decode_join_kernel joins what belongs together, in the order of the keys: who ran a piece changes nothing. The lengths are read on the device, so a captured call follows them.
 //
-// A thread block. One warp plans ahead: lengths, page table, the q rows of every unit. One thread loads the tiles into a ring. Eight
+// A thread block. One warp plans ahead: lengths, page table, the q rows of every unit. One loads the tiles into a ring. Eight
 // warps, two sets of four, take 16 rows of a tile each, one head's, with a running maximum, sum and O of their own (the sets take
 // tiles in turn, or, with more than eight query heads per K / V head, each half of the query heads). When a unit is through they
 // leave them in shared memory and each joins some of the query heads, while the ring goes on being filled.
@@ -49,7 +49,7 @@ struct __align__(16) UnitDesc {
     int32_t seq, unit;                      // unit of the sequence
     int32_t slot;                           // of a partial result; negative: the whole unit is here
 };
-// What the planning warp hands to the loading thread at a time: up to eight tiles of one unit. (No more of them: the pieces that a
+// What the planning warp hands to the loading warp at a time: up to eight tiles of one unit. (No more of them: the pieces that a
 // block pops are to depend on how far it is.)
 constexpr int kBatches = 2, kBatchTiles = 8;
 struct __align__(16) BatchDesc {
@@ -308,7 +308,7 @@ hydra_decode_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_cons
 
     if (warp == S::kConsumers) {
         // ------------------------------------------------------------------ pieces, page table, q
-        // Runs ahead of the loading thread, which must not wait for anything but places in the ring: what it does not issue for a
+        // Runs ahead of the loading warp, which must not wait for anything but places in the ring: what it does not issue for a
         // moment, the memory does not catch up on.
         if (p.debug_stall_ns) {
             debug_stall(p.debug_stall_ns);              // test hook: plan nothing; the other warps' waits run out
@@ -398,56 +398,68 @@ hydra_decode_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_cons
         }
     } else if (warp == S::kConsumers + 1) {
         // ------------------------------------------------------------------ loads
-        if (elect_one()) {
-            const int32_t box_rows = p.box_rows, boxes = p.boxes;
-            const uint32_t row_bytes = static_cast<uint32_t>(p.unit_kv_heads) * (kDqk + D_V) * 2;      // of a key
-            const uint32_t k_box = static_cast<uint32_t>(box_rows * p.unit_kv_heads) * kDqk * 2, v_box = static_cast<uint32_t>(box_rows * p.unit_kv_heads) * D_V * 2;
-            uint32_t st = 0, turn = 0;                  // place in the ring
-            bool ok = true;
-            for (uint32_t n_batch = 0; ok; ++n_batch) {
-                const uint32_t at = n_batch % kBatches;
-                ok = wait(B_BFULL + at, n_batch / kBatches);
-                if (!ok) break;
-                const BatchDesc batch = s_batch[at];
-                if (batch.tiles < 0) {
-                    if (wait(B_EMPTY + st, turn ^ 1u)) {
-                        s_tile[st].unit = kEnd;
-                        mbar_arrive(bar(B_FULL + st));
-                    }
-                    break;
+        // The lanes issue the copies of a tile's boxes side by side: 128 us for 300 sequences of 1500 tokens, two K / V heads of 128, on
+        // pages of 8 tokens (eight boxes per tile, 3.6 TB/s), one thread alone 180 us; the same with one or two boxes per tile.
+        const int32_t box_rows = p.box_rows, boxes = p.boxes;
+        const uint32_t row_bytes = static_cast<uint32_t>(p.unit_kv_heads) * (kDqk + D_V) * 2;      // of a key
+        const uint32_t k_box = static_cast<uint32_t>(box_rows * p.unit_kv_heads) * kDqk * 2, v_box = static_cast<uint32_t>(box_rows * p.unit_kv_heads) * D_V * 2;
+        const int32_t of_tile = lane / boxes, j = lane - of_tile * boxes;       // this lane's box: the tile of the batch, its number in the tile
+        uint32_t st = 0, turn = 0;                  // place in the ring
+        for (uint32_t n_batch = 0;; ++n_batch) {
+            const uint32_t at = n_batch % kBatches;
+            if (!wait_together(B_BFULL + at, n_batch / kBatches)) break;
+            const BatchDesc batch = s_batch[at];
+            const BoxDesc d = s_box[at][lane];
+            if (batch.tiles < 0) {
+                if (wait_together(B_EMPTY + st, turn ^ 1u) && lane == 0) {
+                    s_tile[st].unit = kEnd;
+                    mbar_arrive(bar(B_FULL + st));
                 }
-                for (int32_t i = 0; i < batch.tiles; ++i) {
-                    BoxDesc d = s_box[at][i * boxes];
-                    ok = wait(B_EMPTY + st, turn ^ 1u);
-                    if (!ok) break;
-                    const uint32_t full = bar(B_FULL + st);
-                    uint32_t k_dst = ring + st * S::kStage, v_dst = k_dst + S::kKBytes;
-                    uint64_t seen = 0;
+                break;
+            }
+            mbar_arrive_warp(bar(B_BEMPTY + at));
+            const uint64_t seen = d.page < 0 ? 0ull : (~0ull >> (64 - d.rows)) << (j * box_rows);
+            const int32_t pieces = d.page < 0 || d.rows > box_rows - 8 ? 0 : (d.rows + 7) / 8;     // of eight rows; 0: the whole box
+            uint32_t lo = static_cast<uint32_t>(seen), hi = static_cast<uint32_t>(seen >> 32);
+            for (int x = 1; x < boxes; x *= 2) {
+                lo |= __shfl_xor_sync(0xffffffffu, lo, x);
+                hi |= __shfl_xor_sync(0xffffffffu, hi, x);
+            }
+            bool ok = true;
+            for (int32_t i = 0; i < batch.tiles; ++i) {
+                ok = wait_together(B_EMPTY + st, turn ^ 1u);
+                if (!ok) break;
+                const uint32_t full = bar(B_FULL + st);
+                if (of_tile == i && j == 0) {
                     mbar_expect_tx(full, d.loaded * row_bytes);
-                    for (int32_t j = 0; j < boxes; ++j, k_dst += k_box, v_dst += v_box) {
-                        if (j) d = s_box[at][i * boxes + j];
-                        if (d.page < 0) continue;
-                        seen |= (~0ull >> (64 - d.rows)) << (j * box_rows);
-                        if (d.rows == box_rows) {
-                            tma_load_5d(k_dst, &map_k, full, 0, 0, d.row, batch.head, d.page);
-                            tma_load_5d(v_dst, &map_v, full, 0, 0, d.row, batch.head, d.page);
-                        } else {                        // the last rows of a sequence: eight at a time, head by head
-                            for (int32_t h = 0; h < p.unit_kv_heads; ++h)
-                                for (int32_t r = 0; r < d.rows; r += 8) {
-                                    const uint32_t to = static_cast<uint32_t>(h * box_rows + r);
-                                    tma_load_5d(k_dst + to * kDqk * 2, &map_k8, full, 0, 0, d.row + r, batch.head + h, d.page);
-                                    tma_load_5d(v_dst + to * D_V * 2, &map_v8, full, 0, 0, d.row + r, batch.head + h, d.page);
-                                }
-                        }
-                    }
-                    s_tile[st].seen = seen;
+                    s_tile[st].seen = static_cast<uint64_t>(hi) << 32 | lo;
                     s_tile[st].unit = batch.unit | (batch.left - i == 1 ? kLastOfUnit : 0u);
                     s_tile[st].set = (batch.set + i) % S::kTurns;
-                    mbar_arrive(full);
-                    if (++st == S::kStages) { st = 0; ++turn; }
                 }
-                mbar_arrive(bar(B_BEMPTY + at));
+                __syncwarp();
+                if (of_tile == i && d.page >= 0) {
+                    const uint32_t k_dst = ring + st * S::kStage + j * k_box, v_dst = ring + st * S::kStage + S::kKBytes + j * v_box;
+                    if (pieces == 0) {
+                        tma_load_5d(k_dst, &map_k, full, 0, 0, d.row, batch.head, d.page);
+                        tma_load_5d(v_dst, &map_v, full, 0, 0, d.row, batch.head, d.page);
+                    }
+                }
+                // a sequence's last rows, where they need not a whole box: eight at a time, head by head
+                if (const uint32_t cut = __ballot_sync(0xffffffffu, of_tile == i && pieces > 0)) {
+                    const int32_t from = __ffs(cut) - 1, n = __shfl_sync(0xffffffffu, pieces, from), box = from - i * boxes;
+                    const int32_t row = __shfl_sync(0xffffffffu, d.row, from), page = __shfl_sync(0xffffffffu, d.page, from);
+                    const int32_t h = lane / n, r = (lane - h * n) * 8;
+                    if (h < p.unit_kv_heads) {
+                        const uint32_t to = static_cast<uint32_t>((box * p.unit_kv_heads + h) * box_rows + r);
+                        tma_load_5d(ring + st * S::kStage + to * kDqk * 2, &map_k8, full, 0, 0, row + r, batch.head + h, page);
+                        tma_load_5d(ring + st * S::kStage + S::kKBytes + to * D_V * 2, &map_v8, full, 0, 0, row + r, batch.head + h, page);
+                    }
+                }
+                __syncwarp();
+                if (of_tile == i && j == 0) mbar_arrive(full);
+                if (++st == S::kStages) { st = 0; ++turn; }
             }
+            if (!ok) break;
         }
     } else {
         // ------------------------------------------------------------------ scores, softmax, O
