@@ -75,7 +75,10 @@ struct Shape {
     static constexpr int kConsumers = 2 * kSlices;                      // warps
     static constexpr int kThreads = 32 * (kConsumers + 2);
     static constexpr int kKBytes = kTileRows * kDqk * 2, kVBytes = kTileRows * D_V * 2, kStage = kKBytes + kVBytes;
-    static constexpr int kQBytes = (kRows + kWarpRows) * kDqk * 2;      // (the last rows that a product takes may be padding)
+    // Bytes between rows of q: eight rows meet all banks. (Without the 16 they met the same four: eight warps' matrix loads took some
+    // 1000 cycles per unit. One sequence of 1000 tokens 12.3 -> 10.9 us, 19 of a 32K batch 65.9 -> 63.5, 230 of 64 to 512 tokens 211 -> 208.)
+    static constexpr int kQRow = kDqk * 2 + 16;
+    static constexpr int kQBytes = (kRows == 32 ? kRows : kRows + kWarpRows) * kQRow;  // (the last rows that a product takes may be padding)
     // floats between rows of the join buffer: 2 * 132 = 8 (mod 32), the eight values and four heads of a warp's store meet 32 banks
     static constexpr int kJoinStride = D_V + 4;
     static constexpr int kJoinBytes = kConsumers * kWarpRows * kJoinStride * 4;
@@ -340,18 +343,18 @@ hydra_decode_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_cons
                     // ------------------------------------------------ a unit's tiles in this piece: q rows, what the joining warp needs
                     int32_t left = min(n_tiles - tile, hi - t);
                     const int32_t end = t += left;
+                    const int32_t q_slot = n_unit % S::kQSlots, rows = p.rows_of(unit);
                     if (lane == 0) {
-                        const int32_t q_slot = n_unit % S::kQSlots, head0 = p.first_head(unit), rows = p.rows_of(unit);
                         ok = wait(B_QEMPTY + q_slot, (n_unit / S::kQSlots) ^ 1u);
                         if (ok) {
                             s_unit[q_slot] = {b, unit, left < n_tiles ? 2 * piece + (tile == 0 ? 1 : 0) : -1};
                             mbar_arrive_expect_tx(bar(B_QFULL + q_slot), static_cast<uint32_t>(rows) * kDqk * 2);
-                            bulk_load(q_ring + static_cast<uint32_t>(q_slot) * S::kQBytes,
-                                      p.q + b * p.q_stride + static_cast<int64_t>(head0) * kDqk,
-                                      static_cast<uint32_t>(rows) * kDqk * 2, bar(B_QFULL + q_slot));
                         }
                     }
                     ok = __shfl_sync(0xffffffffu, ok, 0);
+                    if (ok && lane < rows)
+                        bulk_load(q_ring + static_cast<uint32_t>(q_slot) * S::kQBytes + lane * S::kQRow,
+                                  p.q + b * p.q_stride + static_cast<int64_t>(p.first_head(unit) + lane) * kDqk, kDqk * 2, bar(B_QFULL + q_slot));
                     while (left > 0 && ok) {
                         const int32_t n = min(left, most), key = (tile << p.tile_shift) + lane * box_rows;
                         const int32_t rows = lane < n * boxes ? min(box_rows, len - key) : 0;
@@ -508,7 +511,7 @@ hydra_decode_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_cons
 #pragma unroll
                 for (int t = 0; t < kNT; ++t) {
                     const uint32_t q_at = q_ring + static_cast<uint32_t>(q_slot) * S::kQBytes +
-                                          static_cast<uint32_t>(q_row + t * 8 + (lane & 7)) * (kDqk * 2) + (lane >> 3) * 16;
+                                          static_cast<uint32_t>(q_row + t * 8 + (lane & 7)) * S::kQRow + (lane >> 3) * 16;
 #pragma unroll
                     for (int ks = 0; ks < kDqk / 16; ks += 2) {
                         uint32_t f[4];
@@ -516,8 +519,8 @@ hydra_decode_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_cons
                         q[ks][t][0] = f[0]; q[ks][t][1] = f[1]; q[ks + 1][t][0] = f[2]; q[ks + 1][t][1] = f[3];
                     }
                 }
-                // Nothing has used the loaded rows yet. Without the fence an asynchronous copy of the slot's next unit can be ahead of
-                // the last of these loads, as one of the units of one tile or two was in some ten calls of a share of 32.
+                // Nothing has waited for the loads of the rows yet. Without the fence they can still be on their way when an asynchronous
+                // copy of a later unit's rows lands in the slot, as happened with short units in one of some ten calls.
                 fence_proxy_async_smem();
                 mbar_arrive_warp(bar(B_QEMPTY + q_slot));
 #pragma unroll
