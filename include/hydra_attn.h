@@ -504,8 +504,8 @@ int32_t hydra_gate_apply_bwd(const void* dy, const void* out, const void* gate, 
  *   >= n_heads * head_dim: x may be a slice of a fused projection's output); positions device int32 [n_axes, n_tokens].
  *   inverse != 0 rotates by the opposite angles: the gradient of the step. y == x (with equal strides) rotates in place;
  *   otherwise the two must not overlap, and the other columns are copied.
- * One launch on cuda_stream, bound by HBM: every byte moves once (in place: the rotary ones). fp32 arithmetic, angles in double precision,
- * one rounding per element.
+ * One launch on cuda_stream, bound by HBM: every byte moves once (in place: the rotary ones). fp32 arithmetic, angles in
+ * double precision, one rounding per element.
  * Requirements: head_dim <= 1024, offset, dim <= 256 and the strides multiples of 8 elements, n_heads <= 65536, x and y 16-byte
  * aligned (else HYDRA_ERR_UNSUPPORTED for the multiples and limits, HYDRA_ERR_INVALID_ARG for pointers); theta > 1.
  */
@@ -534,6 +534,8 @@ int32_t hydra_rope_axes(const void* x, int64_t x_stride, const int32_t* position
  * The struct is host memory, read during the call. Lengths, table and cache contents are read on the device when the kernels
  * run: a captured call follows them, and neither call waits for the device or copies to the host.
  *
+ * The rows that an append reads must not lie in the cache; out, lse and the workspace of the attention overlap nothing else.
+ *
  * hydra_kv_append: token t of the n_tokens rows of k, v is one of the new tokens of a sequence: of sequence b for cu_new[b] <=
  * t < cu_new[b + 1], and with n = cu_new[b + 1] - cu_new[b] new tokens it is token seq_lens[b] - n + (t - cu_new[b]) of that
  * sequence. Its key row of every head is rotated as by hydra_rope_axes and stored, its value row stored; all other rows of the cache
@@ -551,18 +553,19 @@ int32_t hydra_rope_axes(const void* x, int64_t x_stride, const int32_t* position
  * One launch each, bound by HBM: every byte moves once. Requirements: as for hydra_rope_axes, with d_qk and d_v <= 1024
  * multiples of 8 and a k_pe stride that is even (k_pe 4-byte aligned).
  *
- * hydra_attn_decode: for every sequence b and query head a,
- *   s_j = softmax_scale * <q[b, a], k_j> over the positions j < seq_lens[b] whose page is there, of KV head a / (n_heads /
- *   n_kv_heads);  lse[a, b] = ln sum_j exp(s_j),  out[b, a] = sum_j exp(s_j - lse) v_j   (no position: out = 0, lse = -inf).
+ * hydra_attn_decode: for every sequence b and query head a, over the positions j < seq_lens[b] whose page is there,
+ *   s_j = softmax_scale * <q[b, a], k_j>   (k_j and v_j of KV head a / (n_heads / n_kv_heads)),
+ *   lse[a, b] = ln sum_j exp(s_j),  out[b, a] = sum_j exp(s_j - lse) v_j   (no position: out = 0, lse = -inf).
  *   q           device bf16: head a of sequence b at element b * q_stride + a * d_qk (q_stride a multiple of 8).
  *   out, lse    device bf16 [n_seqs, n_heads, d_v], fp32 [n_heads, n_seqs]: an (out, lse) as of hydra_attn_fwd, with n_seqs
  *               tokens; hydra_lse_merge_accumulate merges it with others.
  *   workspace   device, >= hydra_workspace_bytes_decode(n_heads, n_kv_heads) bytes, 16-byte aligned; whatever it held before.
  * Cached rows that do not count (behind a sequence's end, on pages of others) may hold anything, infinities and NaN too; q and
- * the rows that count must be finite. Scores, softmax and sums in fp32, probabilities enter the product with v in 16 bits of precision, one
- * rounding of out; the result does not depend on timing, and the sequences' lengths decide how the work is split.
- * Two launches. (d_qk, d_v) = (192, 128) or (128, 128), page_size a multiple of 8, max_pages * page_size <= 2^30, and the n_seqs
- * rows of the table hold no more than 2^30 blocks of 16 keys and KV head (else HYDRA_ERR_UNSUPPORTED). A wait in the kernel that runs out leaves HYDRA_ERR_DEVICE_TIMEOUT in the workspace's status.
+ * the rows that count must be finite. Scores, softmax and sums in fp32, probabilities enter the product with v in 16 bits of
+ * precision, one rounding of out; the result does not depend on timing, and the sequences' lengths decide how the work is split.
+ * Two launches (one more that clears the status where they are recorded). (d_qk, d_v) = (192, 128) or (128, 128), page_size a
+ * multiple of 8, max_pages * page_size <= 2^30, and the n_seqs rows of the table hold no more than 2^30 blocks of 16 keys and KV
+ * head (else HYDRA_ERR_UNSUPPORTED). A wait in the kernel that runs out leaves HYDRA_ERR_DEVICE_TIMEOUT in the workspace's status.
  */
 typedef struct hydra_paged_cache_t {
     void *k, *v;
@@ -585,7 +588,8 @@ int32_t hydra_attn_decode(const void* q, int64_t q_stride, const hydra_paged_cac
  * Per-kernel timing (measurement aid, not part of the method). While enabled, every kernel launch
  * is bracketed by CUDA events on its stream. hydra_profile_collect waits for the recorded events,
  * adds their durations into ms_out[8] and their counts into launches_out[8] (index: 0 forward, both of its
- * kernels when a call uses both, and hydra_attn_decode, 1 merge, and the join of hydra_attn_decode, 2 backward prep, 3 backward dK/dV, 4 backward dQ, 5 gradient cast, 6 Ulysses pack / unpack,
+ * kernels when a call uses both, and hydra_attn_decode, 1 merge, and the join of hydra_attn_decode,
+ * 2 backward prep, 3 backward dK/dV, 4 backward dQ, 5 gradient cast, 6 Ulysses pack / unpack,
  * 7 the elementwise steps of the gated MLA block, hydra_rope_axes and the appends to a paged cache)
  * and forgets them.
  */
