@@ -8,7 +8,8 @@ import torch
 import hydra_workloads as hw
 import oracle
 from gpu_util import TOL_LSE, TOL_REL
-from paged_util import DV, THETA, bits, dev, f64, i32, scattered_table, to_bits
+from oracle import paged_cache as C
+from paged_util import DV, THETA, bits, check_decode, decode_bounds, dev, f64, i32, scattered_table, to_bits
 
 pytestmark = pytest.mark.gpu
 
@@ -96,3 +97,44 @@ def test_prefill_and_steps(h, hk, d, mla, axes, captured):
             ref_o, ref_l = oracle.attn_fwd_gqa(qb, kb, vb, hw.cu_seqlens([length]), True, np.float32(scale))
             assert np.abs(f64(o1[b]) - ref_o[-1]).max() <= 2.0 ** -8 * np.abs(ref_o[-1]).max() + 1e-3
             assert np.abs(l1[:, b].cpu().numpy() - ref_l[:, -1]).max() <= TOL_LSE
+
+
+def test_pages_behind_the_first_2_32_elements():
+    """The last pages of a cache whose K alone has 4.3e9 elements (8.6 GB): what the appends store there, the attention reads."""
+    import paper_2609_34318_b200 as P
+    rng = np.random.default_rng(17)
+    hk, h, d, page, lengths = 4, 8, 192, 64, [130, 1, 70]
+    n_pages = 2 ** 32 // (hk * page * d) + 8
+    kp = torch.empty(n_pages, hk, page, d, dtype=torch.bfloat16, device="cuda")
+    vp = torch.empty(n_pages, hk, page, DV, dtype=torch.bfloat16, device="cuda")
+    assert kp.numel() > 2 ** 32 and vp.numel() > 2 ** 31
+    small, used = scattered_table(lengths, page, rng, spare=0)
+    table = np.where(small < 0, -1, n_pages - 1 - small).astype(np.int32)
+    T = sum(lengths)
+    kb, vb, qb = bits(rng, T, hk, d), bits(rng, T, hk, DV), bits(rng, 3, h, d)
+    cu = np.concatenate([[0], np.cumsum(lengths)]).astype(np.int32)
+    cache = P.paged_cache(kp, vp, i32(table), i32(lengths))
+    P.hydra_kv_append(dev(kb), dev(vb), None, i32(cu), T, None, cache)
+    up, pe = bits(rng, 1, hk, 128 + DV), bits(rng, 1, 64)           # the last token of the third sequence once more, from the MLA form
+    P.hydra_mla_kv_append(dev(up), dev(pe), None, i32([0, 0, 0, 1]), 1, P.rope_spec(THETA, 64, 128), cache)
+    out, lse = torch.empty(3, h, DV, dtype=torch.bfloat16, device="cuda"), torch.empty(h, 3, device="cuda")
+    ws = torch.zeros(P.hydra_workspace_bytes_decode(h, hk), dtype=torch.uint8, device="cuda")
+    scale = float(np.float32(d ** -0.5))
+    P.hydra_attn_decode(dev(qb), cache, h, scale, out, lse, ws)
+    assert P.hydra_poll_status(ws) == (0, -1)
+    last = torch.arange(used, device="cuda").neg() + n_pages - 1
+    k, v = f64(kp[last]), f64(vp[last])             # page p of the small table
+    for b in range(3):
+        for j in range(lengths[b] - (b == 2)):
+            at, row = small[b][j // page], j % page
+            assert np.array_equal(k[at, :, row], hw.bf16_bits_to_f64(kb[cu[b] + j])) and np.array_equal(v[at, :, row], hw.bf16_bits_to_f64(vb[cu[b] + j]))
+    row = k[small[2][69 // page], :, 69 % page]
+    assert np.array_equal(row[:, :128], hw.bf16_bits_to_f64(up)[0, :, :128]) and (row[:, 128:] == row[:1, 128:]).all()
+    q = hw.bf16_bits_to_f64(qb)
+    count = np.zeros_like(k[:, :1, :, :1])
+    for b in range(3):
+        for j in range(lengths[b]):
+            count[small[b][j // page], :, j % page] = 1
+    k, v = np.where(count > 0, k, 0.0), np.where(count > 0, v, 0.0)
+    ref = C.decode(q, k, v, small, np.array(lengths, dtype=np.int32), scale)
+    check_decode(out, lse, *ref, *decode_bounds(q, k, small, lengths, scale, np.abs(v).max()))
