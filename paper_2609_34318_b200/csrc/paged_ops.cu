@@ -23,9 +23,9 @@ constexpr int kPlaceWarps = 8;              // of a block
 constexpr int kMaxTokens = 16;              // that a warp takes at once
 constexpr int kMaxAngles = 512;             // tokens times rotary pairs
 constexpr int kMaxPairs = 128;
-// Vectors of a thread at a time, blocks per SM: more in flight per thread, or fewer and larger warps' shares, were no faster (32K
-// prompt tokens of 16 MLA heads 112 us, 5.4 TB/s; a step of 230 tokens 4.8 us; 65536 patches of a video, two heads of 128, 35 us, of
-// which 8 are their angles and the rotation's products; their 16 query heads rotated 90 us, 6.0 TB/s).
+// Vectors of a thread at a time, blocks per SM. 32K prompt tokens of 16 MLA heads take 112 us (5.4 TB/s), with five blocks (48
+// registers) 130, with six 137; more vectors in flight gained nothing. A step of 230 tokens 4.8 us; 65536 patches of a video, two heads
+// of 128, 35 us, of which 8 are their angles and the rotation's products; their 16 query heads rotated 90 us (6.0 TB/s).
 constexpr int kInFlight = 1;
 constexpr int kPlaceBlocks = 4;
 
@@ -250,7 +250,8 @@ PlaceParams place_params(int64_t n_tokens, int32_t n_heads, const hydra_rope_t* 
     const int32_t elems = 2 * words, rot_elems = rope ? rope->dim : 0, pairs = rot_elems / 2;
     const int32_t per_head = (row_elems + v_elems) / elems;
     // Some eight vectors per thread of a warp: several tokens where they are short, part of the heads where they are long. But
-    // with few tokens the work is spread over the warps of all SMs first, down to two vectors per thread.
+    // with few tokens the work is spread over the warps of all SMs first, down to two vectors per thread. (Half as many: 115 us for
+    // the prompts above and 92 for the video's queries; four times as many: 130 and 96.)
     constexpr int64_t kWarps = 148 * kPlaceWarps * 2, kVectors = 32 * 8;
     int64_t tokens = std::min<int64_t>({kVectors / (int64_t{n_heads} * per_head), n_tokens / kWarps, kMaxTokens});
     if (pairs) tokens = std::min<int64_t>(tokens, kMaxAngles / pairs);
