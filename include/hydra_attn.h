@@ -502,8 +502,8 @@ int32_t hydra_gate_apply_bwd(const void* dy, const void* out, const void* gate, 
  *   rotated as by hydra_mla_rope, bit for bit.
  *   x device bf16, y device bf16: the row of head a of token t begins at element t * stride + a * head_dim (x_stride, y_stride
  *   >= n_heads * head_dim: x may be a slice of a fused projection's output); positions device int32 [n_axes, n_tokens].
- *   inverse != 0 rotates by the opposite angles: the gradient of the step. y == x (with equal strides) rotates in place;
- *   otherwise the two must not overlap, and the other columns are copied.
+ *   inverse != 0 rotates by the opposite angles: the gradient of the step. y == x rotates in place (more than one
+ *   token: with equal strides); otherwise the two must not overlap, and the other columns are copied.
  * One launch on cuda_stream, bound by HBM: every byte moves once (in place: the rotary ones). fp32 arithmetic, angles in
  * double precision, one rounding per element.
  * Requirements: head_dim <= 1024, offset, dim <= 256 and the strides multiples of 8 elements, n_heads <= 65536, x and y 16-byte

@@ -7,6 +7,7 @@ Tensors are torch CUDA tensors (used for device memory and streams only) or raw 
 from __future__ import annotations
 
 import ctypes
+import math
 import os
 from typing import Iterable, Optional, Sequence, Tuple
 
@@ -695,7 +696,8 @@ def hydra_gate_apply_bwd(dy, out, gate, n_elements: int, d_out, d_gate, stream=N
 
 def _rows(x, stride: Optional[int]) -> Tuple[Optional[int], int]:
     """(device pointer, elements between tokens) of rows that are contiguous but for the distance between tokens: a tensor
-    [tokens, ...], possibly a slice of a wider one, or a raw pointer with its stride."""
+    [tokens, ...], possibly a slice of a wider one, or a raw pointer with its stride. Of a single token torch's stride says
+    nothing (a transposed [heads, 1, d] has d there): the row's own length stands for it."""
     if x is None or isinstance(x, int):
         return x, 0 if stride is None else stride
     if not x.is_cuda:
@@ -707,7 +709,9 @@ def _rows(x, stride: Optional[int]) -> Tuple[Optional[int], int]:
             if size != 1 and step != want:
                 raise ValueError("a token's rows must be contiguous")
             want *= size
-    return x.data_ptr(), steps[0] if stride is None else stride
+    if stride is None:
+        stride = steps[0] if x.shape[0] > 1 else math.prod(x.shape[1:])
+    return x.data_ptr(), stride
 
 
 def _spec(x) -> Optional[int]:

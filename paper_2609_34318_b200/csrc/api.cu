@@ -2961,7 +2961,7 @@ int32_t hydra_rope_axes(const void* x, int64_t x_stride, const int32_t* position
     const int32_t bad = check_rope(rope, head_dim);
     if (bad == HYDRA_ERR_INVALID_ARG) return bad;
     const int64_t row = int64_t{n_heads} * head_dim;
-    if (x_stride < row || y_stride < row || (x == y && x_stride != y_stride)) return HYDRA_ERR_INVALID_ARG;
+    if (x_stride < row || y_stride < row || (x == y && n_tokens > 1 && x_stride != y_stride)) return HYDRA_ERR_INVALID_ARG;
     if (bad || head_dim % 8 || head_dim > kMaxPlacedDim || n_heads > kMaxPlacedHeads || x_stride % 8 || y_stride % 8)
         return HYDRA_ERR_UNSUPPORTED;
     if (n_tokens == 0) return HYDRA_OK;
