@@ -1,0 +1,55 @@
+"""Padded batches: any number of rows without a key, or without a new token, between two that have some. What they cost does not
+grow with their number as a walk from row to row would (a dependent load each)."""
+import numpy as np
+import pytest
+import torch
+
+import paper_2609_34318_b200 as P
+from oracle import paged_cache as C
+from paged_util import DV, bits, check_decode, decode_bounds, dev, i32
+
+import hydra_workloads as hw
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.mark.parametrize("empty", [0, 1, 31, 40, 1000, 1 << 18])
+@pytest.mark.parametrize("units", [1, 3])
+def test_a_piece_goes_on_behind_empty_rows(empty, units):
+    """148 shares of two or more tiles, one of which ends a sequence and begins the next one that has keys. With 2^18 empty rows in
+    between a dependent load for each of them takes 60 ms or more, longer than the other warps wait here."""
+    rng = np.random.default_rng(empty + units)
+    d, page, hk = 128, 64, units                    # one K / V head a unit (an odd number of them), tiles of 64 keys
+    lengths = [64 * 149 - 5, 64 * 2 + 9, 64]
+    rows = [empty, 2 * empty + 1, 2 * empty + 2]
+    n = 3 * empty + 3                               # empty rows in front, between the first two, and behind
+    need = [-(-x // page) for x in lengths]
+    ids = rng.permutation(sum(need) + 2).astype(np.int32)
+    small = np.full((3, max(need)), -1, dtype=np.int32)
+    for i, (b, m) in enumerate(zip(rows, need)):
+        small[i, :m], ids = ids[:m], ids[m:]
+    qb, kb, vb = bits(rng, 3, hk, d), bits(rng, sum(need) + 2, hk, page, d), bits(rng, sum(need) + 2, hk, page, DV)
+    table = torch.full((n, max(need)), -1, dtype=torch.int32, device="cuda")
+    lens, q = torch.zeros(n, dtype=torch.int32, device="cuda"), torch.zeros(n, hk, d, dtype=torch.bfloat16, device="cuda")
+    table[rows], lens[rows], q[rows] = i32(small), i32(lengths), dev(qb)
+    out = torch.full((n, hk, DV), float("nan"), dtype=torch.bfloat16, device="cuda")
+    lse = torch.full((hk, n), float("nan"), device="cuda")
+    ws = torch.zeros(P.hydra_workspace_bytes_decode(hk, hk), dtype=torch.uint8, device="cuda")
+    cache = P.paged_cache(dev(kb), dev(vb), table, lens)
+    scale = float(np.float32(d ** -0.5))
+    P.hydra_attn_decode(q, cache, hk, scale, out, lse, ws)      # (what a device does once comes before the short waits)
+    torch.cuda.synchronize()
+    out.fill_(float("nan")), lse.fill_(float("nan"))
+    P.hydra_set_wait_limit_ns(20_000_000)
+    try:
+        P.hydra_attn_decode(q, cache, hk, scale, out, lse, ws)
+        status = P.hydra_poll_status(ws)
+    finally:
+        P.hydra_set_wait_limit_ns(2_000_000_000)
+    assert status == (0, -1)
+    qf, kf, vf = (hw.bf16_bits_to_f64(x) for x in (qb, kb, vb))
+    ref = C.decode(qf, kf, vf, small, np.array(lengths), scale)
+    check_decode(out[rows], lse[:, rows], *ref, *decode_bounds(qf, kf, small, np.array(lengths), scale, np.abs(vf).max()))
+    rest = torch.ones(n, dtype=torch.bool, device="cuda")
+    rest[rows] = False
+    assert not out[rest].any() and torch.isneginf(lse[:, rest]).all()
