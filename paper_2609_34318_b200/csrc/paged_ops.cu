@@ -122,8 +122,20 @@ hydra_place_rows_kernel(const PlaceParams p)
             if (p.cu_new) {
                 b = sequence_of(p.cu_new, p.n_seqs, t0, lane);
                 if (lane < static_cast<int>(n_tok)) {
+                    // A lane's token is of the same sequence as the first or of one close behind, but for rows that append
+                    // nothing: any number of those may lie between, and after a few steps the rest is searched by halves.
                     int32_t end = p.cu_new[b + 1];
-                    while (t >= end && b + 1 < p.n_seqs) end = p.cu_new[++b + 1];      // (a few short sequences further at most)
+                    for (int step = 0; t >= end && b + 1 < p.n_seqs; ++step) {
+                        if (step == kMaxTokens) {
+                            for (int32_t hi = p.n_seqs; hi - b > 1;) {
+                                const int32_t mid = b + (hi - b) / 2;
+                                (p.cu_new[mid] <= t ? b : hi) = mid;
+                            }
+                            end = p.cu_new[b + 1];
+                            break;
+                        }
+                        end = p.cu_new[++b + 1];
+                    }
                     if (t >= p.cu_new[b] && t < end) place = static_cast<int64_t>(p.seq_lens[b]) - (end - t);
                 }
             } else if (lane < static_cast<int>(n_tok) && t < p.n_seqs) {
