@@ -339,13 +339,19 @@ hydra_decode_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_cons
                 ++n_batch;
             };
             auto plan = [&](int32_t piece, int32_t lo, int32_t hi) {
-                int32_t b, before, len;
-                lengths.find(p, lane, p.by_units(lo), b, len, before);
-                int32_t n_tiles = tiles_of(p, len);
-                const int32_t in_seq = lo - before * p.units;
-                int32_t unit = in_seq / n_tiles, tile = in_seq - unit * n_tiles;        // of the sequence, of the unit
+                int32_t b = 0, len = 0, n_tiles = 0, unit = 0, tile = 0;                // unit of the sequence, tile of the unit
                 if (lane == 0) p.arrived[piece] = 0;    // (for the join, which counts with it)
                 for (int32_t t = lo; t < hi && ok;) {
+                    // The sequence is looked up at the piece's beginning and behind a row without a key. Of those there may be any number:
+                    // one after the other, each would be a load that the next one waits for (262144 of them: the call took 42.7 ms, 2.6 so).
+                    if (n_tiles == 0) {
+                        int32_t before;
+                        lengths.find(p, lane, p.by_units(t), b, len, before);
+                        n_tiles = tiles_of(p, len);
+                        const int32_t in_seq = t - before * p.units;
+                        unit = in_seq / n_tiles;
+                        tile = in_seq - unit * n_tiles;
+                    }
                     // ------------------------------------------------ a unit's tiles in this piece: q rows, what the joining warp needs
                     int32_t left = min(n_tiles - tile, hi - t);
                     const int32_t end = t += left;
@@ -385,9 +391,6 @@ hydra_decode_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_cons
                         if (++unit == p.units && t < hi) {
                             unit = 0;
                             len = seq_len_of(p, ++b);
-                            // Rows without a key, of which there may be any number: one after the other, each would be a load that
-                            // the next one waits for (262144 of them: the call took 42.7 ms, 2.5 so).
-                            if (len == 0) lengths.find(p, lane, p.by_units(t), b, len, before);
                             n_tiles = tiles_of(p, len);
                         }
                     }
