@@ -563,7 +563,8 @@ int32_t hydra_rope_axes(const void* x, int64_t x_stride, const int32_t* position
  * Cached rows that do not count (behind a sequence's end, on pages of others) may hold anything, infinities and NaN too; q and
  * the rows that count must be finite. Scores, softmax and sums in fp32, probabilities enter the product with v in 16 bits of
  * precision, one rounding of out; the result does not depend on timing, and the sequences' lengths decide how the work is split.
- * Two launches (one more that clears the status where they are recorded). (d_qk, d_v) = (192, 128) or (128, 128), page_size a
+ * Two launches (one more that clears the status where they are recorded; without a sequence only that one). (d_qk, d_v) = (192, 128)
+ * or (128, 128), page_size a
  * multiple of 8, max_pages * page_size <= 2^30, and the n_seqs rows of the table hold no more than 2^30 blocks of 16 keys and KV
  * head (else HYDRA_ERR_UNSUPPORTED). A wait in the kernel that runs out leaves HYDRA_ERR_DEVICE_TIMEOUT in the workspace's status.
  */

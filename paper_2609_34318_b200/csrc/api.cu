@@ -3036,8 +3036,9 @@ int32_t hydra_attn_decode(const void* q, int64_t q_stride, const hydra_paged_cac
     }
     int sms = 0;
     if (int32_t s = device_info(&sms)) return s;
-    if (c.n_seqs == 0) return HYDRA_OK;
     cudaStream_t stream = static_cast<cudaStream_t>(cuda_stream);
+    if (c.n_seqs == 0)                                  // nothing to do, but the workspace may hold another call's status
+        return launch_reset(static_cast<StatusBlock*>(workspace), false, stream) == cudaSuccess ? HYDRA_OK : HYDRA_ERR_CUDA;
     p.q = static_cast<const uint16_t*>(q);
     p.q_stride = q_stride;
     p.page_table = c.page_table;
