@@ -563,10 +563,12 @@ int32_t hydra_rope_axes(const void* x, int64_t x_stride, const int32_t* position
  * Cached rows that do not count (behind a sequence's end, on pages of others) may hold anything, infinities and NaN too; q and
  * the rows that count must be finite. Scores, softmax and sums in fp32, probabilities enter the product with v in 16 bits of
  * precision, one rounding of out; the result does not depend on timing, and the sequences' lengths decide how the work is split.
- * Two launches (one more that clears the status where they are recorded; without a sequence only that one). (d_qk, d_v) = (192, 128)
- * or (128, 128), page_size a
- * multiple of 8, max_pages * page_size <= 2^30, and the n_seqs rows of the table hold no more than 2^30 blocks of 16 keys and KV
- * head (else HYDRA_ERR_UNSUPPORTED). A wait in the kernel that runs out leaves HYDRA_ERR_DEVICE_TIMEOUT in the workspace's status.
+ * Two launches (one more that clears the status where they are recorded; without a sequence only that one).
+ * (d_qk, d_v) = (192, 128) or (128, 128), page_size a multiple of 8, max_pages * page_size <= 2^30, n_seqs * n_heads < 2^31, and fewer than
+ * 2^30 tiles in a full table: (max_pages * page_size * m / 64 + 1) * n_seqs * u, where m, of 4, 2 and 1, is the most K / V heads that
+ * n_kv_heads is a multiple of and that have no more than 16 query heads together (else 1), and u = n_kv_heads / m, times the query
+ * heads per K / V head in groups of 32 (else HYDRA_ERR_UNSUPPORTED). A wait in the kernel that runs out leaves
+ * HYDRA_ERR_DEVICE_TIMEOUT in the workspace's status.
  */
 typedef struct hydra_paged_cache_t {
     void *k, *v;
