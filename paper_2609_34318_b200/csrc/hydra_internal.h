@@ -344,10 +344,6 @@ struct DecodeParams {
     {
         return chunks == 1 ? unit_rows : min(unit_rows, group - unit % chunks * unit_rows);
     }
-    __device__ __forceinline__ int32_t unit_of(int32_t head) const
-    {
-        return chunks == 1 ? head / unit_rows : head / group * chunks + head % group / unit_rows;
-    }
 #endif
     float scale_log2;           // softmax_scale * log2(e)
     StatusBlock* status;

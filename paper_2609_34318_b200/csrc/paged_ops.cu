@@ -23,10 +23,9 @@ constexpr int kPlaceWarps = 8;              // of a block
 constexpr int kMaxTokens = 16;              // that a warp takes at once
 constexpr int kMaxAngles = 512;             // tokens times rotary pairs
 constexpr int kMaxPairs = 128;
-// Vectors of a thread at a time, blocks per SM. 32K prompt tokens of 16 MLA heads take 112 us (5.4 TB/s), with five blocks (48
-// registers) 130, with six 137; more vectors in flight gained nothing. A step of 230 tokens 4.8 us; 65536 patches of a video, two heads
-// of 128, 35 us, of which 8 are their angles and the rotation's products; their 16 query heads rotated 90 us (6.0 TB/s).
-constexpr int kInFlight = 1;
+// Blocks per SM. 32K prompt tokens of 16 MLA heads take 112 us (5.4 TB/s), with five blocks (48 registers) 130, with six 137; a
+// thread moves a vector at a time, more of them in flight gained nothing. A step of 230 tokens 4.8 us; 65536 patches of a video, two
+// heads of 128, 35 us, of which 8 are their angles and the rotation's products; their 16 query heads rotated 90 us (6.0 TB/s).
 constexpr int kPlaceBlocks = 4;
 
 // Strides, offsets and columns in vectors of 2 kWords elements.
@@ -99,10 +98,9 @@ hydra_place_rows_kernel(const PlaceParams p)
             const uint32_t c = e - p.by_k_row(e) * p.k_vecs;
             return c >= static_cast<uint32_t>(p.rot0) && c < static_cast<uint32_t>(p.rot0 + p.rot_vecs);
         };
-        Words<kWords> first[kInFlight];
-#pragma unroll
-        for (int u = 0; u < kInFlight; ++u)
-            if (const uint32_t e = lane + 32 * u; e < n_k && rotary(e)) first[u] = load_k(e);
+        const bool has_first = static_cast<uint32_t>(lane) < n_k && rotary(lane);
+        Words<kWords> first;
+        if (has_first) first = load_k(lane);
         int32_t position[HYDRA_MAX_AXES * kMaxTokens / 32];
         const uint32_t n_positions = p.positions ? n_tok * p.axes : 0;
 #pragma unroll
@@ -210,34 +208,15 @@ hydra_place_rows_kernel(const PlaceParams p)
                 st_words<kWords>(p.y, at, w);
             }
         };
-#pragma unroll
-        for (int u = 0; u < kInFlight; ++u)
-            if (const uint32_t e = lane + 32 * u; e < n_k && rotary(e)) store_k(e, first[u]);
-        for (uint32_t e0 = lane + 32 * kInFlight; e0 < n_k; e0 += 32 * kInFlight) {
-            Words<kWords> w[kInFlight];
-#pragma unroll
-            for (int u = 0; u < kInFlight; ++u)
-                if (const uint32_t e = e0 + 32 * u; e < n_k && rotary(e)) w[u] = load_k(e);
-#pragma unroll
-            for (int u = 0; u < kInFlight; ++u)
-                if (const uint32_t e = e0 + 32 * u; e < n_k && rotary(e)) store_k(e, w[u]);
-        }
+        if (has_first) store_k(lane, first);
+        for (uint32_t e = lane + 32; e < n_k; e += 32)
+            if (rotary(e)) store_k(e, load_k(e));
         if (kMode == PLACE_KV) {                        // rows of v
             const uint32_t n_v = n_tok * n_heads * p.v_vecs;
-            for (uint32_t e0 = lane; e0 < n_v; e0 += 32 * kInFlight) {
-                Words<kWords> w[kInFlight];
-#pragma unroll
-                for (int u = 0; u < kInFlight; ++u)
-                    if (const uint32_t e = e0 + 32 * u; e < n_v) {
-                        const uint32_t tok = p.by_v_token(e);
-                        w[u] = ld_words<kWords>(p.v, (t0 + tok) * p.v_stride + static_cast<int64_t>(head0) * p.v_vecs + (e - tok * p.by_v_token.d));
-                    }
-#pragma unroll
-                for (int u = 0; u < kInFlight; ++u)
-                    if (const uint32_t e = e0 + 32 * u; e < n_v) {
-                        const uint32_t tok = p.by_v_token(e), in = e - tok * p.by_v_token.d, head = p.by_v_row(in);
-                        if (const int64_t at = to_v(tok, head, in - head * p.v_vecs); at >= 0) st_words<kWords>(p.y_v, at, w[u]);
-                    }
+            for (uint32_t e = lane; e < n_v; e += 32) {
+                const uint32_t tok = p.by_v_token(e), in = e - tok * p.by_v_token.d, head = p.by_v_row(in);
+                const auto w = ld_words<kWords>(p.v, (t0 + tok) * p.v_stride + static_cast<int64_t>(head0) * p.v_vecs + in);
+                if (const int64_t at = to_v(tok, head, in - head * p.v_vecs); at >= 0) st_words<kWords>(p.y_v, at, w);
             }
         }
         if (kMode == PLACE_MLA) {                       // the turned key, for every head
