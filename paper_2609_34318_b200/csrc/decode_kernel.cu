@@ -19,13 +19,15 @@
 // warps, two sets of four, take 16 rows of a tile each, one head's, with a running maximum, sum and O of their own (the sets take
 // tiles in turn, or, with more than eight query heads per K / V head, each half of the query heads). When a unit is through they
 // leave them in shared memory and each joins some of the query heads, while the ring goes on being filled.
-// Products on mma.sync: eight query heads against 16 keys are far below what a tcgen05 product computes at once, and the
-// tensor cores idle either way (1 to 16 FLOP per byte).
+// Products on mma.sync: up to eight query heads per K / V head the loads bound the kernel (the tensor pipe is active for 8 % of the
+// time with eight) and the accumulators stay in the registers that rescale them. From 16 on the products bound it; 128 keys against
+// 8 to 64 query heads would be a shape for tcgen05, which this kernel does not have.
 //
-// Measured (16 heads of 192 / 128): 256K tokens 377 us, 7.1 TB/s read; 230 sequences of 64 to 512 tokens 207 us, 6.5 TB/s; 19
-// sequences of a 32K batch 63 us for 345 MB, of which 5 pass before the first tile (lengths, page, load) and 4 for the join; one
-// sequence of 1000 tokens 10.9 us, nearly all of it that chain. On K / V heads of 128 with 1, 8, 16, 32 query heads each, 524288
-// tokens take 326, 331, 378, 505 us (the copy rate gives 327): up to 8 the loads bound it, then the products.
+// Measured (16 heads of 192 / 128, on two GPUs): 256K tokens 377 to 385 us, 7.0 to 7.1 TB/s read; 230 sequences of 64 to 512 tokens
+// 207 to 213 us, 6.3 to 6.5 TB/s; 19 sequences of a 32K batch 63 us for 345 MB, of which 5 pass before the first tile (lengths, page,
+// load) and 4 for the join; one sequence of 1000 tokens 10.9 us, nearly all of it that chain. On K / V heads of 128 with 1, 8, 16, 17,
+// 32, 64 query heads each, 524288 tokens take 329, 331, 382, 494, 503, 968 us (the copy rate gives 327): more than 32 are read once
+// per 32.
 #include <cuda_bf16.h>
 
 #include <algorithm>
@@ -413,8 +415,9 @@ hydra_decode_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_cons
         }
     } else if (warp == S::kConsumers + 1) {
         // ------------------------------------------------------------------ loads
-        // The lanes issue the copies of a tile's boxes side by side: 128 us for 300 sequences of 1500 tokens, two K / V heads of 128, on
-        // pages of 8 tokens (eight boxes per tile, 3.6 TB/s), one thread alone 180 us; the same with one or two boxes per tile.
+        // The lanes issue the copies of a tile's boxes side by side: 121 us for 300 sequences of 1500 tokens, two K / V heads of 128 with 16
+        // query heads each, on pages of 8 tokens (eight boxes per tile), where pages of 16 or 64 take 115; one thread alone took 180 us.
+        // With one or two boxes per tile either way takes the same.
         const int32_t box_rows = p.box_rows, boxes = p.boxes;
         const uint32_t row_bytes = static_cast<uint32_t>(p.unit_kv_heads) * (kDqk + D_V) * 2;      // of a key
         const uint32_t k_box = static_cast<uint32_t>(box_rows * p.unit_kv_heads) * kDqk * 2, v_box = static_cast<uint32_t>(box_rows * p.unit_kv_heads) * D_V * 2;

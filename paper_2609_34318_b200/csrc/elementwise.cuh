@@ -87,7 +87,8 @@ struct Div {
     __device__ __forceinline__ uint32_t operator()(uint32_t n) const { return m ? __umulhi(n, m) : n; }
 };
 
-// cos / sin of position * freq, the angle reduced as in rope_table
+// cos / sin of position * freq, the angle reduced as in rope_table. The reduced angle, up to 2 pi, is rounded to 32 bits (2^-22 at most):
+// that and the single-precision functions leave cosine and sine off by some 2^-21, where the row is rounded to bf16 by 2^-8.
 __device__ __forceinline__ void rope_angle(int32_t pos, double freq, float& cs, float& sn)
 {
     double ang = static_cast<double>(pos) * freq;

@@ -25,7 +25,8 @@ constexpr int kMaxAngles = 512;             // tokens times rotary pairs
 constexpr int kMaxPairs = 128;
 // Blocks per SM. 32K prompt tokens of 16 MLA heads take 112 us (5.4 TB/s), with five blocks (48 registers) 130, with six 137; a
 // thread moves a vector at a time, more of them in flight gained nothing. A step of 230 tokens 4.8 us; 65536 patches of a video, two
-// heads of 128, 35 us, of which 8 are their angles and the rotation's products; their 16 query heads rotated 90 us (6.0 TB/s).
+// heads of 128, 35 us, of which 8 are their angles and the rotation's products; their 16 query heads rotated 90 to 93 us (5.8 to 6.0
+// TB/s); as many tokens of text, whose angles all have to be formed, into two heads of 128, 43 us.
 constexpr int kPlaceBlocks = 4;
 
 // Strides, offsets and columns in vectors of 2 kWords elements.
